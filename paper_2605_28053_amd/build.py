@@ -2,12 +2,13 @@
 
 Usage: ``python -m paper_2605_28053_amd.build`` (or ``build()`` from Python).
 The library holds the host planner/owner table and the HIP kernels behind the
-C ABI declared in ``include/rwttt.h``.
+C ABI declared in ``include/rwttt.h`` and ``include/rwttt_kv.h``.
 """
 
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -37,17 +38,13 @@ def _run(cmd):
 def build(verbose=False):
     objdir = os.path.join(PKG, "_build")
     os.makedirs(objdir, exist_ok=True)
-    k_obj = os.path.join(objdir, "rwttt_kernels.o")
-    d_obj = os.path.join(objdir, "rwttt_adapter.o")
-    a_obj = os.path.join(objdir, "rwttt_api.o")
-    _run([HIPCC, "-c", f"--offload-arch={ARCH}", *COMMON, *DEVICE_FLAGS,
-          os.path.join(CSRC, "rwttt_kernels.hip"), "-o", k_obj])
-    _run([HIPCC, "-c", f"--offload-arch={ARCH}", *COMMON, *DEVICE_FLAGS,
-          os.path.join(CSRC, "rwttt_adapter.hip"), "-o", d_obj])
-    _run([HIPCC, "-c", f"--offload-arch={ARCH}", *COMMON, *DEVICE_FLAGS,
-          os.path.join(CSRC, "rwttt_api.cpp"), "-o", a_obj])
+    sources = ("rwttt_kernels.hip", "rwttt_adapter.hip", "rwttt_kv.hip", "rwttt_api.cpp", "rwttt_kv_api.cpp")
+    objs = [os.path.join(objdir, os.path.splitext(s)[0] + ".o") for s in sources]
+    with ThreadPoolExecutor(len(sources)) as pool:
+        list(pool.map(lambda so: _run([HIPCC, "-c", f"--offload-arch={ARCH}", *COMMON, *DEVICE_FLAGS,
+                                       os.path.join(CSRC, so[0]), "-o", so[1]]), zip(sources, objs)))
     tmp = LIB + ".tmp"
-    _run([HIPCC, "-shared", f"--offload-arch={ARCH}", "-fPIC", a_obj, k_obj, d_obj, "-o", tmp])
+    _run([HIPCC, "-shared", f"--offload-arch={ARCH}", "-fPIC", *objs, "-o", tmp])
     os.replace(tmp, LIB)
     if verbose:
         print("built", LIB)

@@ -1,0 +1,1159 @@
+// Kernels of the owners' paged key-value cache (include/rwttt_kv.h) for
+// gfx950: block tables and slot maps, stored rows with key bounds per page,
+// page selection, and one new token's attention.
+
+#include "rwttt_kv_kernels.h"
+
+#include <type_traits>
+
+namespace rwttt {
+namespace {
+
+#include "rwttt_device.h"
+
+typedef const __attribute__((address_space(4))) int32_t* scalar_i32;   // read through the scalar cache
+
+__device__ __forceinline__ scalar_i32 scalar(const int32_t* p) {
+  return reinterpret_cast<scalar_i32>(reinterpret_cast<uintptr_t>(p));
+}
+
+__device__ __forceinline__ int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }
+
+// Inclusive sum over a wave's lanes.
+__device__ __forceinline__ int wave_scan(int x) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int y = __shfl_up(x, d);
+    if (lane >= d) x += y;
+  }
+  return x;
+}
+
+// ---------------------------------------------------------------------------
+// extend: lengths -> pages, table, slots
+// ---------------------------------------------------------------------------
+//
+// The three prefix sums over the owners (pages taken, pages returned, new rows)
+// fix every output, so each block computes them itself -- 8 bytes an owner, from
+// the L2 -- and then fills its part of the flattened lists by a binary search:
+// one launch, no block waits for another.
+
+constexpr int kExtThreads = 256;
+constexpr int kExtItems = 2048;          // list entries a block fills
+
+struct ExtendSums {
+  int take[RWTTT_KV_MAX_OWNERS + 1];
+  int give[RWTTT_KV_MAX_OWNERS + 1];
+  int add[RWTTT_KV_MAX_OWNERS + 1];
+};
+
+// Last owner whose exclusive sum is <= i (owners without entries are passed over).
+__device__ __forceinline__ int owner_of(const int* sums, int n, int i) {
+  int lo = 0, hi = n;                    // sums[lo] <= i < sums[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (sums[mid] <= i) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+__global__ void __launch_bounds__(kExtThreads) kv_extend_kernel(const KvExtendLaunch p) {
+  extern __shared__ int ext_lds[];
+  const int n = p.s.n_owners, shift = p.s.page_shift, P = 1 << shift;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int* take = ext_lds;
+  int* give = take + n + 1;
+  int* add = give + n + 1;
+  __shared__ long long wave_sum[kExtThreads / 64][3];
+  __shared__ int any_bad;
+  if (tid == 0) any_bad = 0;
+  __syncthreads();
+
+  const int limit = p.s.max_pages << shift;
+  const int per = (n + kExtThreads - 1) / kExtThreads, i0 = min(n, tid * per), i1 = min(n, i0 + per);
+  long long t = 0, g = 0, a = 0;
+  int bad = 0;
+  for (int i = i0; i < i1; ++i) {
+    int h = p.have[i], w = p.want[i];
+    bad |= h < 0 || w < 0 || h > limit || w > limit;
+    h = clampi(h, 0, limit);
+    w = clampi(w, 0, limit);
+    const int ph = (h + P - 1) >> shift, pw = (w + P - 1) >> shift;
+    t += max(0, pw - ph);
+    g += max(0, ph - pw);
+    a += max(0, w - h);
+  }
+  // exclusive sums over the threads, in 64 bits: the totals decide whether the step fits
+  long long st = t, sg = g, sa = a;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const long long x = __shfl_up(st, d), y = __shfl_up(sg, d), z = __shfl_up(sa, d);
+    if (lane >= d) {
+      st += x;
+      sg += y;
+      sa += z;
+    }
+  }
+  if (lane == 63) {
+    wave_sum[wave][0] = st;
+    wave_sum[wave][1] = sg;
+    wave_sum[wave][2] = sa;
+  }
+  if (bad) any_bad = 1;
+  __syncthreads();
+  long long bt = st - t, bg = sg - g, ba = sa - a, taken = 0, given = 0, added = 0;
+  for (int w = 0; w < kExtThreads / 64; ++w) {
+    if (w < wave) {
+      bt += wave_sum[w][0];
+      bg += wave_sum[w][1];
+      ba += wave_sum[w][2];
+    }
+    taken += wave_sum[w][0];
+    given += wave_sum[w][1];
+    added += wave_sum[w][2];
+  }
+  const int front = p.pos[0], count = p.pos[1], pages = p.s.n_pages;
+  int code = RWTTT_OK;
+  if (any_bad || front < 0 || front >= pages || count < 0 || count > pages) code = RWTTT_E_INVALID;
+  else if (taken > count || added > p.cap) code = RWTTT_E_CAPACITY;
+  else if (count - taken + given > pages) code = RWTTT_E_INVALID;   // more pages than there are
+  const bool ok = code == RWTTT_OK;
+  if (ok) {
+    for (int i = i0; i < i1; ++i) {
+      const int h = p.have[i], w = p.want[i];
+      const int ph = (h + P - 1) >> shift, pw = (w + P - 1) >> shift;
+      take[i] = int(bt);
+      give[i] = int(bg);
+      add[i] = int(ba);
+      bt += max(0, pw - ph);
+      bg += max(0, ph - pw);
+      ba += max(0, w - h);
+    }
+    if (tid == 0) {
+      take[n] = int(taken);
+      give[n] = int(given);
+      add[n] = int(added);
+    }
+  }
+  __syncthreads();
+
+  const int b = blockIdx.x, step = gridDim.x * kExtThreads, at = b * kExtThreads + tid;
+  for (int i = at; i < n + 1; i += step) {
+    if (i < n) p.lengths[i] = ok ? p.want[i] : p.have[i];
+    p.start[i] = ok ? add[i] : 0;
+  }
+  if (at == 0) {
+    p.new_pos[0] = ok ? int((front + taken) % pages) : front;
+    p.new_pos[1] = ok ? int(count - taken + given) : count;
+    p.result[0] = code;
+    p.result[1] = ok ? int(added) : 0;
+    p.result[2] = ok ? int(taken) : 0;
+    p.result[3] = ok ? int(given) : 0;
+  }
+  auto ring_at = [&](long long i) { return int((front + i) % pages); };
+  if (ok) {
+    for (int i = at; i < taken; i += step) {
+      const int r = owner_of(take, n, i);
+      const int ph = (p.have[r] + P - 1) >> shift;
+      p.table[size_t(r) * p.s.max_pages + ph + (i - take[r])] = p.ring[ring_at(i)];
+    }
+    for (int i = at; i < given; i += step) {
+      const int r = owner_of(give, n, i);
+      const int pw = (p.want[r] + P - 1) >> shift;
+      p.ring[ring_at((long long)count + i)] = p.table[size_t(r) * p.s.max_pages + pw + (i - give[r])];
+    }
+  }
+  for (long long i = at; i < p.cap; i += step) {
+    int slot = -1, owner = -1, position = -1;
+    if (ok && i < added) {
+      const int r = owner_of(add, n, int(i));
+      const int h = p.have[r], ph = (h + P - 1) >> shift;
+      owner = r;
+      position = h + (int(i) - add[r]);
+      const int lp = position >> shift;
+      // a page taken in this call comes from the ring: its table entry may not be written yet
+      const int page = lp >= ph ? p.ring[ring_at(take[r] + (lp - ph))] : p.table[size_t(r) * p.s.max_pages + lp];
+      if (unsigned(page) < unsigned(pages)) slot = (page << shift) + (position & (P - 1));
+    }
+    p.slots[i] = slot;
+    p.owners[i] = owner;
+    p.positions[i] = position;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// append: new rows through the slots, with the pages' key bounds
+// ---------------------------------------------------------------------------
+//
+// A wave takes one kv head of a run of tokens, keys or values.  Sixteen bytes a
+// lane: LPR lanes hold a row, 64 / LPR rows go by in one instruction.  Value
+// waves copy their kAppendRun tokens.  A key wave owns the pages that begin in
+// its run (their first token in this call does): it follows each to its last
+// token, so one wave sees all of a page's new keys and the bounds need no
+// atomics.
+
+// To e4m3 of two values already scaled, clamped to the largest number; NaN stays.
+__device__ __forceinline__ float fp8_clamp(float x) { return x != x ? x : fminf(fmaxf(x, -448.f), 448.f); }
+
+template <int IO, int CT> struct AppendRow {   // 16 bytes of io
+  static constexpr int E = IO ? 8 : 4;
+  float x[E];            // stored values, in the cache's own units
+  __device__ __forceinline__ void load(const char* src, float inv_scale) {
+    const u32x4_t w = *reinterpret_cast<const u32x4_t*>(src);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (IO) {
+        x[2 * i] = bf16_lo(w[i]);
+        x[2 * i + 1] = bf16_hi(w[i]);
+      } else {
+        x[i] = __uint_as_float(w[i]);
+      }
+    }
+    if constexpr (CT == RWTTT_FP8) {
+#pragma unroll
+      for (int i = 0; i < E; ++i) x[i] = fp8_clamp(x[i] * inv_scale);
+    }
+  }
+  // Store E values at dst and leave in x what the cache then holds.
+  __device__ __forceinline__ void store(char* dst) {
+    if constexpr (CT == RWTTT_F32) {
+      *reinterpret_cast<f32x4_t*>(dst) = (f32x4_t){x[0], x[1], x[2], x[3]};
+    } else if constexpr (CT == RWTTT_BF16) {
+      uint32_t w[E / 2];
+#pragma unroll
+      for (int i = 0; i < E / 2; ++i) {
+        w[i] = bf16x2_rne(x[2 * i], x[2 * i + 1]);
+        x[2 * i] = bf16_lo(w[i]);
+        x[2 * i + 1] = bf16_hi(w[i]);
+      }
+      if constexpr (E == 8) *reinterpret_cast<u32x4_t*>(dst) = (u32x4_t){w[0], w[1], w[2], w[3]};
+      else *reinterpret_cast<u32x2_t*>(dst) = (u32x2_t){w[0], w[1]};
+    } else {
+      uint32_t w[E / 4];
+#pragma unroll
+      for (int i = 0; i < E / 4; ++i) {
+        int v = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i], x[4 * i + 1], 0, false);
+        v = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 2], x[4 * i + 3], v, true);
+        w[i] = uint32_t(v);
+        x[4 * i] = __builtin_amdgcn_cvt_f32_fp8(v, 0);
+        x[4 * i + 1] = __builtin_amdgcn_cvt_f32_fp8(v, 1);
+        x[4 * i + 2] = __builtin_amdgcn_cvt_f32_fp8(v, 2);
+        x[4 * i + 3] = __builtin_amdgcn_cvt_f32_fp8(v, 3);
+      }
+      if constexpr (E == 8) *reinterpret_cast<u32x2_t*>(dst) = (u32x2_t){w[0], w[1]};
+      else *reinterpret_cast<uint32_t*>(dst) = w[0];
+    }
+  }
+};
+
+struct AppendParams {
+  KvAppendLaunch L;
+  int run;               // tokens a wave looks at
+};
+
+template <int IO, int CT, int D>
+__global__ void __launch_bounds__(256) kv_append_kernel(const AppendParams ap) {
+  const KvAppendLaunch& p = ap.L;
+  constexpr int IOB = IO ? 2 : 4, CB = CT == RWTTT_F32 ? 4 : CT == RWTTT_BF16 ? 2 : 1;
+  using Row = AppendRow<IO, CT>;
+  constexpr int E = Row::E, LPR = D / E, RPI = 64 / LPR;
+  const int lane = threadIdx.x & 63;
+  const int unit = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int H = p.s.kv_heads, shift = p.s.page_shift, P = 1 << shift;
+  const int h = unit % H, is_v = (unit / H) & 1;
+  const int t0 = (unit / H >> 1) * ap.run, n = int(p.n), t1 = min(n, t0 + ap.run);
+  if (t0 >= n) return;
+  const unsigned rows = unsigned(p.s.n_pages) << shift;
+  const char* src = static_cast<const char*>(is_v ? p.v_new : p.k_new) + size_t(h) * D * IOB;
+  const size_t pitch = (is_v ? p.v_stride : p.k_stride) * IOB;
+  char* cache = static_cast<char*>(is_v ? p.v : p.k);
+  const float* scales = is_v ? p.v_scale : p.k_scale;
+  const float scale = CT == RWTTT_FP8 && scales ? scales[h] : 1.f, inv_scale = 1.f / scale;
+  const int sub = lane / LPR, piece = lane % LPR;
+
+  // Row of the cache -> where the lane's piece goes.
+  auto dst_of = [&](unsigned slot) {
+    return cache + ((size_t(slot >> shift) * H + h) * P + (slot & (P - 1))) * size_t(D * CB) + piece * (E * CB);
+  };
+
+  if (is_v || !p.bounds) {
+    for (int t = t0 + sub; t < t1; t += RPI) {
+      const unsigned slot = unsigned(p.slots[t]);
+      if (slot >= rows) continue;
+      Row r;
+      r.load(src + t * pitch + piece * 16, inv_scale);
+      r.store(dst_of(slot));
+    }
+    return;
+  }
+
+  const float inv_step = 1.f / p.step[h];
+  for (int t = t0; t < t1;) {
+    const unsigned slot = unsigned(p.slots[t]);
+    const unsigned before = t > 0 ? unsigned(p.slots[t - 1]) : ~0u;
+    if (slot >= rows || (before < rows && before >> shift == slot >> shift)) {
+      ++t;               // padded, or a page that an earlier wave (or turn) follows
+      continue;
+    }
+    const unsigned page = slot >> shift;
+    // [t, end): the page's tokens in this call
+    int end = t;
+    bool fresh = false;
+    for (;;) {
+      const unsigned s = end + lane < n ? unsigned(p.slots[end + lane]) : ~0u;
+      const bool same = s < rows && s >> shift == page;
+      const unsigned long long miss = __ballot(!same);
+      const int run = miss ? __builtin_ctzll(miss) : 64;
+      fresh |= __ballot(lane < run && (s & (P - 1)) == 0) != 0;
+      end += run;
+      if (run < 64) break;
+    }
+    float lo[E], hi[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      lo[i] = 127.f;
+      hi[i] = -127.f;
+    }
+    for (int u = t + sub; u < end; u += RPI) {
+      Row r;
+      r.load(src + u * pitch + piece * 16, inv_scale);
+      r.store(dst_of(unsigned(p.slots[u])));
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        const float x = (CT == RWTTT_FP8 ? r.x[i] * scale : r.x[i]) * inv_step;
+        lo[i] = fminf(lo[i], floorf(x));     // a NaN leaves the bound as it is
+        hi[i] = fmaxf(hi[i], ceilf(x));
+      }
+    }
+#pragma unroll
+    for (int d = LPR; d < 64; d <<= 1) {
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        lo[i] = fminf(lo[i], __shfl_xor(lo[i], d));
+        hi[i] = fmaxf(hi[i], __shfl_xor(hi[i], d));
+      }
+    }
+    if (sub == 0) {
+      int8_t* at = p.bounds + (size_t(page) * H + h) * (2 * D) + piece * E;
+      uint32_t wl[E / 4], wh[E / 4];
+#pragma unroll
+      for (int i = 0; i < E / 4; ++i) {
+        wl[i] = fresh ? 0x7f7f7f7fu : reinterpret_cast<const uint32_t*>(at)[i];
+        wh[i] = fresh ? 0x81818181u : reinterpret_cast<const uint32_t*>(at + D)[i];
+        uint32_t nl = 0, nh = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int l = min(int(int8_t(wl[i] >> (8 * j))), int(fmaxf(lo[4 * i + j], -127.f)));
+          const int u = max(int(int8_t(wh[i] >> (8 * j))), int(fminf(hi[4 * i + j], 127.f)));
+          nl |= uint32_t(l & 0xff) << (8 * j);
+          nh |= uint32_t(u & 0xff) << (8 * j);
+        }
+        reinterpret_cast<uint32_t*>(at)[i] = nl;
+        reinterpret_cast<uint32_t*>(at + D)[i] = nh;
+      }
+    }
+    t = end;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// select: the pages with the largest scores
+// ---------------------------------------------------------------------------
+//
+// max(q lo, q hi) is max(q, 0) hi - max(-q, 0) lo, so the group's queries fold
+// into two vectors of whole numbers, U = sum max(q8, 0) and V = sum max(-q8, 0),
+// before any page is read: a page costs two 8-bit dot products.  U and V reach
+// 127 * group, so each is split into two base-128 digits.
+
+constexpr int kSelThreads = 1024;
+
+template <int IO, int D>
+__global__ void __launch_bounds__(kSelThreads) kv_select_kernel(const KvSelectLaunch p) {
+  extern __shared__ uint32_t sel_lds[];
+  const int H = p.s.kv_heads, G = p.s.group, shift = p.s.page_shift, P = 1 << shift;
+  const int i = blockIdx.x / H, h = blockIdx.x % H;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int r = p.rows ? p.rows[i] : i;
+  if (unsigned(r) >= unsigned(p.s.n_owners)) return;
+  const int len = clampi(p.lengths[r], 0, p.s.max_pages << shift);
+  const int np = (len + P - 1) >> shift, keep = int(p.keep);
+  int32_t* out = p.pages + (size_t(r) * H + h) * keep;
+  if (np <= keep) {
+    for (int j = tid; j < keep; j += kSelThreads) out[j] = j < np ? j : -1;
+    return;
+  }
+
+  uint32_t* key = sel_lds;               // [np] scores, ordered as unsigned numbers
+  __shared__ uint32_t digits[4][D / 4];  // U's low and high digit, V's low and high digit
+  __shared__ uint32_t hist[256];
+  __shared__ float wave_max[kSelThreads / 64];
+  __shared__ uint32_t pick[2];
+  __shared__ int wave_cnt[kSelThreads / 64][2];
+
+  // the group's largest magnitude, then its digits
+  float a = 0.f;
+  const size_t q0 = size_t(r) * p.q_stride + size_t(h) * G * D;
+  for (int j = tid; j < G * D; j += kSelThreads) {
+    const float q = IO ? Elem<uint16_t>::get(p.q, q0 + j) : Elem<float>::get(p.q, q0 + j);
+    a = fmaxf(a, fabsf(q));
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) a = fmaxf(a, __shfl_xor(a, d));
+  if (lane == 0) wave_max[wave] = a;
+  __syncthreads();
+  a = 0.f;
+  for (int w = 0; w < kSelThreads / 64; ++w) a = fmaxf(a, wave_max[w]);
+  const float inv = 1.f / a, to = a > 0.f && inv < INFINITY ? inv * 127.f : 0.f;
+  if (tid < D) {
+    int U = 0, V = 0;
+    for (int g = 0; g < G; ++g) {
+      const float q = IO ? Elem<uint16_t>::get(p.q, q0 + g * D + tid) : Elem<float>::get(p.q, q0 + g * D + tid);
+      const int q8 = int(fminf(fmaxf(rintf(q * to), -127.f), 127.f));   // the clamp only acts on NaN
+      U += max(q8, 0);
+      V += max(-q8, 0);
+    }
+    uint8_t* dg = reinterpret_cast<uint8_t*>(digits);
+    dg[tid] = uint8_t(U & 127);
+    dg[D + tid] = uint8_t(U >> 7);
+    dg[2 * D + tid] = uint8_t(V & 127);
+    dg[3 * D + tid] = uint8_t(V >> 7);
+  }
+  __syncthreads();
+
+  // scores: LPP lanes a page, 16 bytes of its bounds each; the first half of
+  // them hold the low bounds
+  constexpr int LPP = 2 * D / 16, PPI = 64 / LPP;
+  const int piece = lane % LPP, sub = lane / LPP;
+  const bool low = piece < LPP / 2;
+  int d0[4], d1[4];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const int at = (piece % (LPP / 2)) * 4 + w;
+    d0[w] = int(digits[low ? 2 : 0][at]);
+    d1[w] = int(digits[low ? 3 : 1][at]);
+  }
+  const int32_t* table = p.table + size_t(r) * p.s.max_pages;
+  for (int j = wave * PPI + sub; j < np; j += (kSelThreads / 64) * PPI) {
+    const unsigned page = min(unsigned(table[j]), unsigned(p.s.n_pages - 1));
+    const u32x4_t b = *reinterpret_cast<const u32x4_t*>(p.bounds + (size_t(page) * H + h) * (2 * D) + piece * 16);
+    int s0 = 0, s1 = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      s0 = __builtin_amdgcn_sdot4(int(b[w]), d0[w], s0, false);
+      s1 = __builtin_amdgcn_sdot4(int(b[w]), d1[w], s1, false);
+    }
+    int s = s0 + (s1 << 7);
+    s = low ? -s : s;
+#pragma unroll
+    for (int d = 1; d < LPP; d <<= 1) s += __shfl_xor(s, d);
+    if (piece == 0) {
+      const bool forced = j < int(p.first) || j >= np - int(p.last);
+      key[j] = forced ? ~0u : uint32_t(s) ^ 0x80000000u;
+    }
+  }
+  __syncthreads();
+
+  // the keep-th largest key, eight bits at a time: `want` of the keys that
+  // share the bits found so far are still to be taken
+  uint32_t prefix = 0, mask = 0;
+  int want = keep;
+  for (int bit = 24; bit >= 0; bit -= 8) {
+    if (tid < 256) hist[tid] = 0;
+    __syncthreads();
+    for (int j = tid; j < np; j += kSelThreads) {
+      const uint32_t k = key[j];
+      if ((k & mask) == prefix) atomicAdd(&hist[(k >> bit) & 255], 1u);
+    }
+    __syncthreads();
+    if (wave == 0) {
+      // lane l holds bins 255 - 4l .. 252 - 4l, from the top
+      int c[4], sum = 0;
+#pragma unroll
+      for (int b = 0; b < 4; ++b) sum += c[b] = int(hist[255 - (4 * lane + b)]);
+      int above = wave_scan(sum) - sum;
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        if (above < want && above + c[b] >= want) {
+          pick[0] = uint32_t(255 - (4 * lane + b));
+          pick[1] = uint32_t(want - above);
+        }
+        above += c[b];
+      }
+    }
+    __syncthreads();
+    prefix |= pick[0] << bit;
+    mask |= 255u << bit;
+    want = int(pick[1]);
+    __syncthreads();
+  }
+
+  // all keys above the threshold and the first `want` equal to it, in order
+  const int per = (np + kSelThreads - 1) / kSelThreads, j0 = min(np, tid * per), j1 = min(np, j0 + per);
+  int over = 0, equal = 0;
+  for (int j = j0; j < j1; ++j) {
+    over += key[j] > prefix;
+    equal += key[j] == prefix;
+  }
+  int so = wave_scan(over), se = wave_scan(equal);
+  if (lane == 63) {
+    wave_cnt[wave][0] = so;
+    wave_cnt[wave][1] = se;
+  }
+  __syncthreads();
+  so -= over;
+  se -= equal;
+  for (int w = 0; w < wave; ++w) {
+    so += wave_cnt[w][0];
+    se += wave_cnt[w][1];
+  }
+  for (int j = j0; j < j1; ++j) {
+    const bool gt = key[j] > prefix, eq = key[j] == prefix;
+    if (gt || (eq && se < want)) out[so + min(se, want)] = j;
+    so += gt;
+    se += eq;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// attend: one new token over the cache
+// ---------------------------------------------------------------------------
+//
+// Bound by the cache's bytes: a key and a value are used by at most sixteen
+// queries.  All work of a call -- tiles of KT rows of every (listed owner, kv
+// head, sixteen queries) -- forms one line that is cut into equal parts, one a
+// wave, so a long owner is spread over the chip and many short ones fill it as
+// well.  A wave needs no other: it keeps the running maximum and sum of its
+// queries and the unscaled output in registers, writes the output of a row it
+// holds whole, and leaves at most two partial rows (one that began before its
+// part, one that ends after it) in the workspace for the join.
+//
+// Matrix instructions with the keys as rows and the queries as columns:
+// S^T = K Q^T (16 x 16 over the head's channels) leaves each lane 4 rows of one
+// query, which is the operand layout of P^T in O^T = V^T P^T when the rows are
+// dealt to the tiles so that a lane's 4 + 4 scores are 8 consecutive rows.  So
+// neither scores nor probabilities move between lanes.  V arrives with the
+// channels of a row in one lane; its transposed operand takes one byte
+// permutation for each pair of values.
+
+constexpr int kAttThreads = 256;
+
+struct AttendParams {
+  KvAttendLaunch L;
+  float* part;           // [waves * 2][heads a wave holds][D]
+  float* part_ml;        // [waves * 2][heads a wave holds][2]: maximum (of log2), sum
+  int waves, head_tiles, part_heads;
+  float scale_log2;      // scale * log2(e)
+};
+
+// Rows of keys a wave takes at a time.
+constexpr int tile_rows(int ct) { return ct == RWTTT_F32 ? 16 : 32; }
+
+struct RowRange {
+  int owner, len, base, tiles, held;     // base: first tile's first row; held: listed pages
+};
+
+template <int KT>
+__device__ __forceinline__ RowRange row_range(const KvAttendLaunch& p, int i) {
+  RowRange x{-1, 0, 0, 0, 0};
+  const int r = p.rows ? p.rows[i] : i;
+  if (unsigned(r) >= unsigned(p.s.n_owners)) return x;
+  x.owner = r;
+  x.len = clampi(p.lengths[r], 0, p.s.max_pages << p.s.page_shift);
+  if (x.len == 0) return x;
+  if (p.pages) {
+    const int np = (x.len + (1 << p.s.page_shift) - 1) >> p.s.page_shift;
+    x.held = min(np, int(p.keep));
+    x.tiles = ((x.held << p.s.page_shift) + KT - 1) / KT;
+  } else {
+    const int lo = p.window ? max(0, x.len - int(p.window)) : 0;
+    x.base = lo / KT * KT;
+    x.tiles = (x.len - x.base + KT - 1) / KT;
+  }
+  return x;
+}
+
+// pre[i] = tiles of the listed owners before i, pre[n] their sum.
+template <int KT>
+__device__ __forceinline__ void scan_tiles(const KvAttendLaunch& p, uint32_t* pre, uint32_t* wave_sum) {
+  const int n = int(p.n), tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int per = (n + kAttThreads - 1) / kAttThreads, i0 = min(n, tid * per), i1 = min(n, i0 + per);
+  uint32_t sum = 0;
+  for (int i = i0; i < i1; ++i) sum += uint32_t(row_range<KT>(p, i).tiles);
+  const uint32_t inc = uint32_t(wave_scan(int(sum)));
+  if (lane == 63) wave_sum[wave] = inc;
+  __syncthreads();
+  uint32_t at = inc - sum;
+  for (int w = 0; w < wave; ++w) at += wave_sum[w];
+  for (int i = i0; i < i1; ++i) {
+    pre[i] = at;
+    at += uint32_t(row_range<KT>(p, i).tiles);
+  }
+  if (i1 == n && i0 < n) pre[n] = at;
+  __syncthreads();
+}
+
+// Part w of [0, total) cut into `parts` parts, the first ones one longer.
+struct Cut {
+  uint64_t per, rem;
+  __device__ Cut(uint64_t total, int parts) : per(total / parts), rem(total % parts) {}
+  __device__ uint64_t begin(uint64_t w) const { return w * per + min(w, rem); }
+  __device__ int part_of(uint64_t u) const {
+    const uint64_t head = rem * (per + 1);
+    return int(u < head ? u / (per + 1) : rem + (u - head) / per);
+  }
+};
+
+__device__ __forceinline__ int parts_of(uint64_t total, int waves) { return int(min(total, uint64_t(waves))); }
+
+template <int W> __device__ __forceinline__ void load_words(const char* p, uint32_t* w) {
+  if constexpr (W == 1) {
+    w[0] = *reinterpret_cast<const uint32_t*>(p);
+  } else if constexpr (W == 2) {
+    const u32x2_t t = *reinterpret_cast<const u32x2_t*>(p);
+    w[0] = t[0];
+    w[1] = t[1];
+  } else {
+    const u32x4_t t = *reinterpret_cast<const u32x4_t*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = t[i];
+  }
+}
+
+__device__ __forceinline__ uint32_t fp8_pair(uint32_t w, bool high) {   // exact: e4m3 fits bf16
+  const bf16x2_t h = high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, true)
+                          : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, false);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+__device__ __forceinline__ bf16x8_t as_bf16x8(const uint32_t* w) {
+  const u32x4_t t = {w[0], w[1], w[2], w[3]};
+  return *reinterpret_cast<const bf16x8_t*>(&t);
+}
+
+// x = terms[0] + terms[1] + ... in bf16, eight values a lane: two terms keep 16
+// bits of each, three all 24.
+template <int N> __device__ __forceinline__ void split_bf16(const float* x, bf16x8_t* terms) {
+  float rest[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) rest[i] = x[i];
+#pragma unroll
+  for (int t = 0; t < N; ++t) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      w[i] = bf16x2_rne(rest[2 * i], rest[2 * i + 1]);
+      if (t + 1 < N) {
+        rest[2 * i] -= bf16_lo(w[i]);
+        rest[2 * i + 1] -= bf16_hi(w[i]);
+      }
+    }
+    terms[t] = as_bf16x8(w);
+  }
+}
+
+// Layout of one tile.  CT: cache type, D: head dim.
+//   keys:   KW 16-byte pieces a lane and 16-row tile; piece s of lane group g
+//           holds the channels from key_channel(s, g) on
+//   values: NE chunks of VE channels a lane, from value_channel(e, c) on, for
+//           each of the KT / 4 rows of the lane's group
+template <int CT, int D> struct TileShape {
+  static constexpr int B = CT == RWTTT_F32 ? 4 : CT == RWTTT_BF16 ? 2 : 1;
+  static constexpr int KT = tile_rows(CT), NT = KT / 16;
+  static constexpr int KE = 16 / B, KW = D / (4 * KE);
+  static constexpr int VE = D / 16 < KE ? D / 16 : KE, NE = D / 16 / VE, VW = VE * B / 4;
+  static constexpr int VR = KT / 4;      // rows of values a lane holds
+  static constexpr int NA = D / 16;      // output tiles (four channels a lane)
+  __device__ static int key_channel(int s, int g) { return (s * 4 + g) * KE; }
+  __device__ static int value_channel(int e, int c) { return (e * 16 + c) * VE; }
+};
+
+// Which pages a tile's halves (16 rows each) lie in, and which of their rows count.
+template <int NT> struct TileAt {
+  uint32_t page[NT];
+  int off[NT], from[NT], to[NT];         // rows [from, to) of the half count
+};
+
+template <int IO, int CT, int D>
+__global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kernel(const AttendParams ap) {
+  using S = TileShape<CT, D>;
+  constexpr int KT = S::KT, NT = S::NT;
+  constexpr bool F = CT == RWTTT_F32;
+  constexpr int NQ = IO ? 1 : 3, NP = IO ? 2 : 3;      // bf16 terms of a query, of a probability
+  const KvAttendLaunch& p = ap.L;
+  __shared__ uint32_t pre[RWTTT_KV_MAX_OWNERS + 1];
+  __shared__ uint32_t wave_sum[kAttThreads / 64];
+  scan_tiles<KT>(p, pre, wave_sum);
+
+  const int n = int(p.n), H = p.s.kv_heads, HT = ap.head_tiles, VH = H * HT, G = p.s.group;
+  const int shift = p.s.page_shift, P = 1 << shift;
+  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(blockIdx.x * (kAttThreads / 64) + (threadIdx.x >> 6));
+  const uint64_t total = uint64_t(pre[n]) * VH;
+  const int parts = parts_of(total, ap.waves);
+  if (w >= parts) return;
+  const Cut cut(total, parts);
+  uint64_t u = cut.begin(w);
+  const uint64_t end = cut.begin(w + 1);
+
+  int i = 0;                             // the listed owner that u lies in
+  for (int hi = n; hi - i > 1;) {
+    const int mid = (i + hi) >> 1;
+    if (uint64_t(pre[mid]) * VH <= u) i = mid;
+    else hi = mid;
+  }
+  i = __builtin_amdgcn_readfirstlane(i);
+
+  while (u < end) {
+    const uint32_t tiles = __builtin_amdgcn_readfirstlane(pre[i + 1] - pre[i]);
+    if (tiles == 0) {
+      ++i;
+      continue;
+    }
+    const uint64_t x = u - uint64_t(pre[i]) * VH;
+    const int vh = __builtin_amdgcn_readfirstlane(int(x / tiles));
+    const int t0 = __builtin_amdgcn_readfirstlane(int(x % tiles));
+    const int t1 = int(min(uint64_t(tiles), t0 + (end - u)));
+    const RowRange row = row_range<KT>(p, i);
+    const int owner = __builtin_amdgcn_readfirstlane(row.owner);
+    const int len = __builtin_amdgcn_readfirstlane(row.len);
+    const int base = __builtin_amdgcn_readfirstlane(row.base);
+    const int held = __builtin_amdgcn_readfirstlane(row.held);
+    const int h = vh / HT, head0 = (vh % HT) * 16, heads = min(16, G - head0);
+    const int least = p.window ? max(0, len - int(p.window)) : 0, last_page = (len - 1) >> shift;
+    const scalar_i32 table = scalar(p.table + size_t(owner) * p.s.max_pages);
+    const scalar_i32 list = scalar(p.pages ? p.pages + (size_t(owner) * H + h) * p.keep : nullptr);
+
+    auto locate = [&](int t) {
+      TileAt<NT> at;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const int row0 = base + t * KT + j * 16;
+        int lp = row0 >> shift;
+        at.off[j] = row0 & (P - 1);
+        bool none = false;
+        if (p.pages) {
+          none = lp >= held;
+          lp = list[min(lp, held - 1)];
+          none = none || unsigned(lp) > unsigned(last_page);
+        }
+        const int pos = (lp << shift) + at.off[j];
+        at.from[j] = clampi(least - pos, 0, 16);
+        at.to[j] = none ? 0 : clampi(len - pos, 0, 16);
+        at.page[j] = min(uint32_t(table[clampi(lp, 0, last_page)]), uint32_t(p.s.n_pages - 1));
+      }
+      return at;
+    };
+
+    // queries: the lane's column is one of them
+    const size_t q_at = size_t(owner) * p.q_stride + (size_t(h) * G + head0 + (c < heads ? c : 0)) * D;
+    bf16x8_t q[F ? 1 : NQ][F ? 1 : D / 32];
+    f32x4_t qf[F ? D / 16 : 1];
+    if constexpr (F) {
+#pragma unroll
+      for (int s = 0; s < D / 16; ++s) {
+        const float* src = static_cast<const float*>(p.q) + q_at + S::key_channel(s, g);
+        qf[s] = *reinterpret_cast<const f32x4_t*>(src);
+        if (c >= heads) qf[s] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+      }
+    } else {
+#pragma unroll
+      for (int s = 0; s < D / 32; ++s) {
+        constexpr int PER = S::KE / 8;                  // operands a piece of keys feeds
+        const int ch = S::key_channel(s / PER, g) + (s % PER) * 8;
+        if constexpr (IO) {
+          uint32_t wd[4];
+          load_words<4>(static_cast<const char*>(p.q) + (q_at + ch) * 2, wd);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) wd[j] = c < heads ? wd[j] : 0u;
+          q[0][s] = as_bf16x8(wd);
+        } else {
+          float f[8];
+          uint32_t wd[8];
+          load_words<4>(static_cast<const char*>(p.q) + (q_at + ch) * 4, wd);
+          load_words<4>(static_cast<const char*>(p.q) + (q_at + ch) * 4 + 16, wd + 4);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) f[j] = c < heads ? __uint_as_float(wd[j]) : 0.f;
+          bf16x8_t terms[NQ];
+          split_bf16<NQ>(f, terms);
+#pragma unroll
+          for (int k = 0; k < NQ; ++k) q[k][s] = terms[k];
+        }
+      }
+    }
+    const float to_log2 = ap.scale_log2 * (CT == RWTTT_FP8 && p.k_scale ? p.k_scale[h] : 1.f);
+
+    float m = -INFINITY, l = 0.f;
+    f32x4_t acc[S::NA];
+#pragma unroll
+    for (int a = 0; a < S::NA; ++a) acc[a] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+
+    uint32_t kw[NT][S::KW][4];
+    uint32_t vw[S::NE][S::VR][S::VW];
+    // row of a half that the lane loads: keys, one a lane; values, VR in turn
+    const int k_half = NT == 2 ? c >> 3 : 0, v_half = NT == 2 ? g >> 1 : 0;
+    auto half_of = [&](const TileAt<NT>& at, const void* cache, int half) {
+      const uint32_t page = NT == 2 && half ? at.page[NT - 1] : at.page[0];
+      const int off = NT == 2 && half ? at.off[NT - 1] : at.off[0];
+      return static_cast<const char*>(cache) + ((size_t(page) * H + h) * P + off) * size_t(D * S::B);
+    };
+    auto load_keys = [&](const TileAt<NT>& at) {
+      const char* src = half_of(at, p.k, k_half);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const int rr = NT == 2 ? ((c >> 2) & 1) * 8 + t * 4 + (c & 3) : c;
+#pragma unroll
+        for (int s = 0; s < S::KW; ++s) load_words<4>(src + (rr * D + S::key_channel(s, g)) * S::B, kw[t][s]);
+      }
+    };
+    auto load_values = [&](const TileAt<NT>& at) {
+      const char* src = half_of(at, p.v, v_half);
+#pragma unroll
+      for (int e = 0; e < S::NE; ++e)
+#pragma unroll
+        for (int k = 0; k < S::VR; ++k) {
+          const int rr = NT == 2 ? (g & 1) * 8 + k : g * 4 + k;
+          load_words<S::VW>(src + (rr * D + S::value_channel(e, c)) * S::B, vw[e][k]);
+        }
+    };
+
+    TileAt<NT> at = locate(t0), next = at;
+    load_keys(at);
+    load_values(at);
+    for (int t = t0; t < t1; ++t) {
+      const bool more = t + 1 < t1;
+      if (more) next = locate(t + 1);
+
+      // scores: s[j] belongs to the tile's row g * VR + j
+      float s[S::VR];
+#pragma unroll
+      for (int k = 0; k < NT; ++k) {
+        f32x4_t sc = {0.f, 0.f, 0.f, 0.f};
+        if constexpr (F) {
+#pragma unroll
+          for (int a = 0; a < D / 16; ++a)
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+              sc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kw[k][a][b]), qf[a][b], sc, 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int a = 0; a < D / 32; ++a) {
+            bf16x8_t key;
+            if constexpr (CT == RWTTT_BF16) {
+              key = as_bf16x8(kw[k][a]);
+            } else {
+              uint32_t wd[4];
+#pragma unroll
+              for (int b = 0; b < 4; ++b) wd[b] = fp8_pair(kw[k][a / 2][(a & 1) * 2 + b / 2], b & 1);
+              key = as_bf16x8(wd);
+            }
+#pragma unroll
+            for (int b = NQ - 1; b >= 0; --b)
+              sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[b][a], sc, 0, 0, 0);
+          }
+        }
+#pragma unroll
+        for (int b = 0; b < 4; ++b) s[k * 4 + b] = sc[b] * to_log2;
+      }
+      if (more) load_keys(next);
+
+      bool whole = true;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) whole = whole && at.from[j] == 0 && at.to[j] == 16;
+      // the lane's rows of its half that count
+      const int from = (v_half ? at.from[NT - 1] : at.from[0]) - (NT == 2 ? (g & 1) * 8 : g * 4);
+      const int to = (v_half ? at.to[NT - 1] : at.to[0]) - (NT == 2 ? (g & 1) * 8 : g * 4);
+      if (!whole) {
+#pragma unroll
+        for (int j = 0; j < S::VR; ++j) s[j] = j >= from && j < to ? s[j] : -INFINITY;
+      }
+      float top = s[0];
+#pragma unroll
+      for (int j = 1; j < S::VR; ++j) top = fmaxf(top, s[j]);
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      if (__any(top > m)) {
+        const float up = fmaxf(m, top), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - up);
+        m = up;
+        l *= f;
+#pragma unroll
+        for (int a = 0; a < S::NA; ++a) acc[a] *= f;
+      }
+      const float ref = m == -INFINITY ? 0.f : m;
+      float pr[S::VR];
+#pragma unroll
+      for (int j = 0; j < S::VR; ++j) {
+        pr[j] = __builtin_amdgcn_exp2f(s[j] - ref);
+        l += pr[j];
+      }
+      if (!whole) {                      // what lies behind an owner's rows may be anything
+#pragma unroll
+        for (int e = 0; e < S::NE; ++e)
+#pragma unroll
+          for (int j = 0; j < S::VR; ++j)
+#pragma unroll
+            for (int b = 0; b < S::VW; ++b) vw[e][j][b] = j >= from && j < to ? vw[e][j][b] : 0u;
+      }
+      if constexpr (F) {
+#pragma unroll
+        for (int e = 0; e < S::NE; ++e)
+#pragma unroll
+          for (int a = 0; a < 4; ++a)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              acc[e * 4 + a] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vw[e][j][a]), pr[j],
+                                                                    acc[e * 4 + a], 0, 0, 0);
+      } else {
+        bf16x8_t pt[NP];
+        split_bf16<NP>(pr, pt);
+#pragma unroll
+        for (int e = 0; e < S::NE; ++e)
+#pragma unroll
+          for (int a = 0; a < S::VE; ++a) {
+            uint32_t wd[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              if constexpr (CT == RWTTT_BF16) {
+                wd[j] = __builtin_amdgcn_perm(vw[e][2 * j + 1][a / 2], vw[e][2 * j][a / 2],
+                                              a & 1 ? 0x07060302u : 0x05040100u);
+              } else {
+                wd[j] = fp8_pair(__builtin_amdgcn_perm(vw[e][2 * j + 1][a / 4], vw[e][2 * j][a / 4],
+                                                       a & 2 ? 0x07030602u : 0x05010400u),
+                                 a & 1);
+              }
+            }
+            const bf16x8_t val = as_bf16x8(wd);
+#pragma unroll
+            for (int b = NP - 1; b >= 0; --b)
+              acc[e * S::VE + a] =
+                  __builtin_amdgcn_mfma_f32_16x16x32_bf16(val, pt[b], acc[e * S::VE + a], 0, 0, 0);
+          }
+      }
+      if (more) {
+        load_values(next);
+        at = next;
+      }
+    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+
+    // acc[e * VE + a][j] is channel value_channel(e, 4 g + j) + a of query c
+    if (t0 == 0 && t1 == int(tiles)) {
+      if (c < heads) {
+        const float vs = CT == RWTTT_FP8 && p.v_scale ? p.v_scale[h] : 1.f;
+        const float norm = l == 0.f ? 0.f : vs / l;
+        const size_t o_at = size_t(owner) * p.out_stride + (size_t(h) * G + head0 + c) * D;
+#pragma unroll
+        for (int e = 0; e < S::NE; ++e)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int a = 0; a < S::VE; a += 4) {
+              const size_t d = o_at + S::value_channel(e, g * 4 + j) + a;
+              const float f0 = acc[e * S::VE + a][j] * norm, f1 = acc[e * S::VE + a + 1][j] * norm;
+              const float f2 = acc[e * S::VE + a + 2][j] * norm, f3 = acc[e * S::VE + a + 3][j] * norm;
+              if constexpr (IO)
+                *reinterpret_cast<u32x2_t*>(static_cast<uint16_t*>(p.out) + d) =
+                    (u32x2_t){bf16x2_rne(f0, f1), bf16x2_rne(f2, f3)};
+              else
+                *reinterpret_cast<f32x4_t*>(static_cast<float*>(p.out) + d) = (f32x4_t){f0, f1, f2, f3};
+            }
+        if (p.lse && g == 0)
+          p.lse[(size_t(owner) * H + h) * G + head0 + c] =
+              l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+      }
+    } else if (c < heads) {
+      const size_t slot = (size_t(w) * 2 + (t0 == 0 ? 1 : 0)) * ap.part_heads + c;
+#pragma unroll
+      for (int e = 0; e < S::NE; ++e)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int a = 0; a < S::VE; a += 4)
+            *reinterpret_cast<f32x4_t*>(ap.part + slot * D + S::value_channel(e, g * 4 + j) + a) =
+                (f32x4_t){acc[e * S::VE + a][j], acc[e * S::VE + a + 1][j], acc[e * S::VE + a + 2][j],
+                          acc[e * S::VE + a + 3][j]};
+      if (g == 0) {
+        ap.part_ml[slot * 2] = m;
+        ap.part_ml[slot * 2 + 1] = l;
+      }
+    }
+    u += uint64_t(t1 - t0);
+    if (t1 == int(tiles) && vh == VH - 1) ++i;
+  }
+}
+
+// Joins the rows that more than one wave worked on, and fills those without
+// keys.  One block a (listed owner, query head): the parts' weights first, then
+// their weighted sum in a fixed order.
+template <int IO, int CT, int D>
+__global__ void __launch_bounds__(kAttThreads) kv_attend_join_kernel(const AttendParams ap) {
+  const KvAttendLaunch& p = ap.L;
+  constexpr int LPR = D / 4, ROWS = kAttThreads / LPR;      // lanes a part, parts in one turn
+  __shared__ uint32_t pre[RWTTT_KV_MAX_OWNERS + 1];
+  __shared__ uint32_t wave_sum[kAttThreads / 64];
+  __shared__ float red[kAttThreads / 64][2];
+  __shared__ f32x4_t sums[ROWS][LPR];
+  scan_tiles<tile_rows(CT)>(p, pre, wave_sum);
+
+  const int n = int(p.n), H = p.s.kv_heads, G = p.s.group, HT = ap.head_tiles, VH = H * HT;
+  const int i = blockIdx.x / (H * G), head = blockIdx.x % (H * G), h = head / G, hg = head % G;
+  const int vh = h * HT + hg / 16, c = hg % 16;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int owner = p.rows ? p.rows[i] : i;
+  if (unsigned(owner) >= unsigned(p.s.n_owners)) return;
+  const uint32_t tiles = pre[i + 1] - pre[i];
+  const size_t o_at = size_t(owner) * p.out_stride + size_t(head) * D;
+  if (tiles == 0) {
+    if (tid < D) {
+      if constexpr (IO) Elem<uint16_t>::put(p.out, o_at + tid, 0.f);
+      else Elem<float>::put(p.out, o_at + tid, 0.f);
+    }
+    if (p.lse && tid == 0) p.lse[size_t(owner) * H * G + head] = -INFINITY;
+    return;
+  }
+  const uint64_t total = uint64_t(pre[n]) * VH;
+  const Cut cut(total, parts_of(total, ap.waves));
+  const uint64_t u0 = uint64_t(pre[i]) * VH + uint64_t(vh) * tiles;
+  const int w0 = cut.part_of(u0), w1 = cut.part_of(u0 + tiles - 1);
+  if (w0 == w1) return;                  // one wave held the row and wrote it
+
+  auto slot_of = [&](int w) { return (size_t(w) * 2 + (w == w0 ? 1 : 0)) * ap.part_heads + c; };
+  float m = -INFINITY;
+  for (int w = w0 + tid; w <= w1; w += kAttThreads) m = fmaxf(m, ap.part_ml[slot_of(w) * 2]);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+  if (lane == 0) red[wave][0] = m;
+  __syncthreads();
+  m = red[0][0];
+  for (int k = 1; k < kAttThreads / 64; ++k) m = fmaxf(m, red[k][0]);
+  const float ref = m == -INFINITY ? 0.f : m;
+
+  const int part = tid / LPR, col = tid % LPR;
+  f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+  float l = 0.f;
+  for (int w = w0 + part; w <= w1; w += ROWS) {
+    const size_t slot = slot_of(w);
+    const float f = __builtin_amdgcn_exp2f(ap.part_ml[slot * 2] - ref);
+    l += f * ap.part_ml[slot * 2 + 1];
+    sum += f * *reinterpret_cast<const f32x4_t*>(ap.part + slot * D + col * 4);
+  }
+  sums[part][col] = sum;
+  __shared__ float ls[ROWS];
+  if (col == 0) ls[part] = l;
+  __syncthreads();
+  if (part == 0) {
+    l = ls[0];
+    for (int k = 1; k < ROWS; ++k) {
+      sum += sums[k][col];
+      l += ls[k];
+    }
+    const float vs = CT == RWTTT_FP8 && p.v_scale ? p.v_scale[h] : 1.f;
+    const float norm = l == 0.f ? 0.f : vs / l;
+    const size_t d = o_at + col * 4;
+    if constexpr (IO)
+      *reinterpret_cast<u32x2_t*>(static_cast<uint16_t*>(p.out) + d) =
+          (u32x2_t){bf16x2_rne(sum[0] * norm, sum[1] * norm), bf16x2_rne(sum[2] * norm, sum[3] * norm)};
+    else
+      *reinterpret_cast<f32x4_t*>(static_cast<float*>(p.out) + d) = sum * norm;
+    if (p.lse && col == 0)
+      p.lse[size_t(owner) * H * G + head] =
+          l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+  }
+}
+
+constexpr int kAttWaves = 2048;          // two blocks of four waves a CU
+
+int part_heads_of(int group) { return group < 16 ? group : 16; }
+
+}  // namespace
+
+size_t kv_workspace_bytes(int group, int head_dim) {
+  const size_t slots = size_t(kAttWaves) * 2 * part_heads_of(group);
+  return (slots * (size_t(head_dim) + 2) * sizeof(float) + 255) / 256 * 256;
+}
+
+hipError_t launch_kv_extend(const KvExtendLaunch& L, hipStream_t stream) {
+  const unsigned blocks = (L.cap + kExtItems - 1) / kExtItems;
+  const size_t lds = size_t(L.s.n_owners + 1) * 3 * sizeof(int);
+  hipLaunchKernelGGL(kv_extend_kernel, dim3(blocks < 1 ? 1 : blocks > 512 ? 512 : blocks), dim3(kExtThreads), lds,
+                     stream, L);
+  return hipGetLastError();
+}
+
+namespace {
+
+template <int IO, int CT> hipError_t append_dims(const AppendParams& p, hipStream_t stream) {
+  const uint64_t runs = (p.L.n + p.run - 1) / p.run;
+  const dim3 grid(unsigned((runs * 2 * p.L.s.kv_heads + 3) / 4)), block(256);
+  if (p.L.s.head_dim == 64) hipLaunchKernelGGL((kv_append_kernel<IO, CT, 64>), grid, block, 0, stream, p);
+  else if (p.L.s.head_dim == 128) hipLaunchKernelGGL((kv_append_kernel<IO, CT, 128>), grid, block, 0, stream, p);
+  else hipLaunchKernelGGL((kv_append_kernel<IO, CT, 256>), grid, block, 0, stream, p);
+  return hipGetLastError();
+}
+
+template <int IO, int CT> hipError_t attend_dims(const AttendParams& p, hipStream_t stream) {
+  const dim3 grid(kAttWaves / (kAttThreads / 64)), block(kAttThreads);
+  const dim3 join(p.L.n * unsigned(p.L.s.kv_heads * p.L.s.group));
+  auto both = [&](auto dim) {
+    constexpr int D = decltype(dim)::value;
+    hipLaunchKernelGGL((kv_attend_kernel<IO, CT, D>), grid, block, 0, stream, p);
+    hipLaunchKernelGGL((kv_attend_join_kernel<IO, CT, D>), join, block, 0, stream, p);
+  };
+  if (p.L.s.head_dim == 64) both(std::integral_constant<int, 64>());
+  else if (p.L.s.head_dim == 128) both(std::integral_constant<int, 128>());
+  else both(std::integral_constant<int, 256>());
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_kv_append(const KvAppendLaunch& L, hipStream_t stream) {
+  AppendParams p{L, L.n <= 1024 ? 1 : 16};
+  if (L.s.io_bf16) return L.s.cache == RWTTT_BF16 ? append_dims<1, RWTTT_BF16>(p, stream)
+                                                  : append_dims<1, RWTTT_FP8>(p, stream);
+  return L.s.cache == RWTTT_F32    ? append_dims<0, RWTTT_F32>(p, stream)
+         : L.s.cache == RWTTT_BF16 ? append_dims<0, RWTTT_BF16>(p, stream)
+                                   : append_dims<0, RWTTT_FP8>(p, stream);
+}
+
+hipError_t launch_kv_select(const KvSelectLaunch& L, hipStream_t stream) {
+  const dim3 grid(L.n * unsigned(L.s.kv_heads)), block(kSelThreads);
+  const size_t lds = size_t(L.s.max_pages) * sizeof(uint32_t);
+  auto go = [&](auto kernel) {
+    // more than 64 KB of the CU's 160 KB has to be asked for
+    if (lds > 48 * 1024) {
+      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                               hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
+      if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(kernel, grid, block, lds, stream, L);
+    return hipGetLastError();
+  };
+  if (L.s.io_bf16)
+    return L.s.head_dim == 64    ? go(kv_select_kernel<1, 64>)
+           : L.s.head_dim == 128 ? go(kv_select_kernel<1, 128>)
+                                 : go(kv_select_kernel<1, 256>);
+  return L.s.head_dim == 64    ? go(kv_select_kernel<0, 64>)
+         : L.s.head_dim == 128 ? go(kv_select_kernel<0, 128>)
+                               : go(kv_select_kernel<0, 256>);
+}
+
+hipError_t launch_kv_attend(const KvAttendLaunch& L, hipStream_t stream) {
+  AttendParams p;
+  p.L = L;
+  p.waves = kAttWaves;
+  p.head_tiles = (L.s.group + 15) / 16;
+  p.part_heads = part_heads_of(L.s.group);
+  p.part = static_cast<float*>(L.workspace);
+  p.part_ml = p.part + size_t(kAttWaves) * 2 * p.part_heads * L.s.head_dim;
+  p.scale_log2 = L.scale * 1.4426950408889634f;
+  if (L.s.io_bf16) return L.s.cache == RWTTT_BF16 ? attend_dims<1, RWTTT_BF16>(p, stream)
+                                                  : attend_dims<1, RWTTT_FP8>(p, stream);
+  return L.s.cache == RWTTT_F32    ? attend_dims<0, RWTTT_F32>(p, stream)
+         : L.s.cache == RWTTT_BF16 ? attend_dims<0, RWTTT_BF16>(p, stream)
+                                   : attend_dims<0, RWTTT_FP8>(p, stream);
+}
+
+}  // namespace rwttt
