@@ -64,7 +64,7 @@ typedef struct rwttt_kv_config {
     uint32_t page_rows;      /* 16, 32, 64, 128 or 256                            */
     uint32_t max_pages;      /* pages an owner may hold: width of the table       */
     uint32_t n_heads;        /* query heads, a multiple of n_kv_heads             */
-    uint32_t n_kv_heads;     /* n_heads / n_kv_heads <= 128                       */
+    uint32_t n_kv_heads;     /* 1..512; n_heads / n_kv_heads <= 128               */
     uint32_t head_dim;       /* 64, 128 or 256                                    */
     int32_t  io_dtype;       /* RWTTT_F32 / RWTTT_BF16: q, new keys and values, out */
     int32_t  cache_dtype;    /* RWTTT_BF16 / RWTTT_FP8, or RWTTT_F32 for fp32 io  */

@@ -26,7 +26,7 @@ rwttt_status check_shape(const rwttt_kv_config* c) {
   if (c->page_rows < 16 || c->page_rows > 256 || (c->page_rows & (c->page_rows - 1))) return RWTTT_E_INVALID;
   if (c->n_pages == 0 || uint64_t(c->n_pages) * c->page_rows > 0x7fffffffu) return RWTTT_E_INVALID;
   if (c->max_pages == 0 || uint64_t(c->max_pages) * c->page_rows > RWTTT_KV_MAX_ROWS) return RWTTT_E_INVALID;
-  if (c->n_kv_heads == 0 || c->n_kv_heads > 1024 || c->n_heads == 0 || c->n_heads % c->n_kv_heads)
+  if (c->n_kv_heads == 0 || c->n_kv_heads > 512 || c->n_heads == 0 || c->n_heads % c->n_kv_heads)
     return RWTTT_E_INVALID;
   if (c->n_heads / c->n_kv_heads > 128) return RWTTT_E_INVALID;
   if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return RWTTT_E_INVALID;
@@ -225,6 +225,7 @@ rwttt_status rwttt_kv_attend(rwttt_kv* kv, uint32_t layer, const void* q, uint64
   L.rows = rows;
   L.pages = pages;
   L.n = n;
+  L.n_layers = kv->cfg.n_layers;
   L.window = window;
   L.keep = keep;
   L.scale = scale;

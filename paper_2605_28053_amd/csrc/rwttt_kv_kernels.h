@@ -50,7 +50,7 @@ struct KvAttendLaunch {
   const float *k_scale, *v_scale;
   uint64_t q_stride, out_stride;
   const int32_t *table, *lengths, *rows, *pages;
-  uint32_t n, window, keep;
+  uint32_t n, n_layers, window, keep;
   float scale;
   void* out;
   float* lse;
