@@ -36,8 +36,8 @@
  *    access outside the caller's buffers: lengths are clamped to
  *    [0, max_pages * page_rows], page ids to [0, n_pages), and such slots are
  *    skipped.  What such rows compute is not specified.
- *  - A handle is read-only for its calls except for its workspace: attends
- *    that may overlap in time need a handle (and workspace) each.
+ *  - A handle is read-only for its calls except for its workspace: attends,
+ *    and selects, that may overlap in time need a handle (and workspace) each.
  */
 #ifndef RWTTT_KV_H
 #define RWTTT_KV_H
@@ -80,17 +80,18 @@ typedef struct rwttt_kv_config {
     const float* k_scale;    /* [n_layers, n_kv_heads]: an 8-bit key times its    */
     const float* v_scale;    /*   head's scale is its value; RWTTT_FP8 only, NULL: 1 */
     const float* bound_step; /* [n_layers, n_kv_heads]: unit of the bounds; needed
-                                with bounds                                       */
+                                with bounds.  Scales and steps are positive and
+                                normal numbers, and so are their reciprocals      */
     void* workspace;         /* rwttt_kv_workspace_bytes() bytes, 256-byte aligned,
                                 all zero when the handle is created (each call
-                                leaves its counters zero); needed by
-                                rwttt_kv_attend                                   */
+                                leaves its counters zero); rwttt_kv_attend needs
+                                it, rwttt_kv_select is faster with it             */
     size_t workspace_bytes;
 } rwttt_kv_config;
 
-/* Bytes of device workspace of a handle: partial results of the attention's
- * splits, a number that the head layout fixes (no length or owner count
- * enters).  Only the shape fields are read. */
+/* Bytes of device workspace of a handle: counters, partial results of the
+ * attention's splits (the head layout fixes their number), and the page scores
+ * of at most 256 (owner, kv head) pairs.  Only the shape fields are read. */
 rwttt_status rwttt_kv_workspace_bytes(const rwttt_kv_config* cfg, size_t* bytes);
 
 /* Create a handle: copies the pointers, makes no HIP call.  RWTTT_E_INVALID

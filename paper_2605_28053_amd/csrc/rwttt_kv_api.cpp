@@ -37,9 +37,21 @@ rwttt_status check_shape(const rwttt_kv_config* c) {
   return RWTTT_OK;
 }
 
-size_t workspace_of(const rwttt_kv_config* c) {
-  return rwttt::kv_workspace_bytes(int(c->n_heads / c->n_kv_heads), int(c->head_dim));
+rwttt::KvShape shape_of(const rwttt_kv_config* c) {
+  rwttt::KvShape h;
+  h.n_owners = int(c->n_owners);
+  h.n_pages = int(c->n_pages);
+  h.page_shift = __builtin_ctz(c->page_rows);
+  h.max_pages = int(c->max_pages);
+  h.kv_heads = int(c->n_kv_heads);
+  h.group = int(c->n_heads / c->n_kv_heads);
+  h.head_dim = int(c->head_dim);
+  h.io_bf16 = c->io_dtype == RWTTT_BF16;
+  h.cache = c->cache_dtype;
+  return h;
 }
+
+size_t workspace_of(const rwttt_kv_config* c) { return rwttt::kv_workspace_bytes(shape_of(c)); }
 
 bool layers_ok(void* const* p, uint32_t n) {
   if (p)
@@ -117,16 +129,7 @@ rwttt_status rwttt_kv_create(const rwttt_kv_config* cfg, rwttt_kv** out) {
     return RWTTT_E_CAPACITY;
   }
   kv->cfg.k = kv->cfg.v = kv->cfg.bounds = nullptr;
-  rwttt::KvShape& h = kv->shape;
-  h.n_owners = int(cfg->n_owners);
-  h.n_pages = int(cfg->n_pages);
-  h.page_shift = __builtin_ctz(cfg->page_rows);
-  h.max_pages = int(cfg->max_pages);
-  h.kv_heads = int(cfg->n_kv_heads);
-  h.group = int(cfg->n_heads / cfg->n_kv_heads);
-  h.head_dim = int(cfg->head_dim);
-  h.io_bf16 = cfg->io_dtype == RWTTT_BF16;
-  h.cache = cfg->cache_dtype;
+  kv->shape = shape_of(cfg);
   *out = kv;
   return RWTTT_OK;
 }
@@ -195,7 +198,8 @@ rwttt_status rwttt_kv_select(rwttt_kv* kv, uint32_t layer, const void* q, uint64
   if (n == 0) return RWTTT_OK;
   const rwttt::KvSelectLaunch L{kv->shape,      q,       q_stride, static_cast<const int8_t*>(kv->bounds[layer]),
                                 kv->cfg.table, lengths, rows,     n,
-                                first,          last,    keep,     pages};
+                                first,          last,    keep,     pages,
+                                kv->cfg.workspace};
   return hip_result(kv, rwttt::launch_kv_select(L, static_cast<hipStream_t>(stream)));
 }
 

@@ -42,6 +42,7 @@ struct KvSelectLaunch {
   const int32_t *table, *lengths, *rows;
   uint32_t n, first, last, keep;
   int32_t* pages;
+  void* workspace;                          // or null
 };
 
 struct KvAttendLaunch {
@@ -57,7 +58,7 @@ struct KvAttendLaunch {
   void* workspace;
 };
 
-size_t kv_workspace_bytes(int group, int head_dim);
+size_t kv_workspace_bytes(const KvShape& shape);
 hipError_t launch_kv_extend(const KvExtendLaunch& L, hipStream_t stream);
 hipError_t launch_kv_append(const KvAppendLaunch& L, hipStream_t stream);
 hipError_t launch_kv_select(const KvSelectLaunch& L, hipStream_t stream);

@@ -38,6 +38,8 @@ class Cache:
     The table's unused entries name pages of other owners and the rows behind an
     owner's length hold NaN: neither may reach a result."""
 
+    no_workspace = False
+
     def __init__(self, lens, H, G, D, page, io, cache, seed=0, max_pages=None, extra_pages=2, std=1.0, n_layers=1,
                  poison=True):
         g = torch.Generator().manual_seed(seed)
@@ -91,8 +93,9 @@ class Cache:
             table=self.table.data_ptr(), ring=self.ring.data_ptr(), k=[self.kd.data_ptr()], v=[self.vd.data_ptr()],
             bounds=[self.bounds.data_ptr()], k_scale=self.k_scale.data_ptr() if fp8 else 0,
             v_scale=self.v_scale.data_ptr() if fp8 else 0, bound_step=self.step.data_ptr())
-        self.ws = torch.zeros(KV.rwttt_kv_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
-        cfg.workspace, cfg.workspace_bytes = self.ws.data_ptr(), self.ws.numel()
+        if not self.no_workspace:
+            self.ws = torch.zeros(KV.rwttt_kv_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+            cfg.workspace, cfg.workspace_bytes = self.ws.data_ptr(), self.ws.numel()
         return KV.rwttt_kv_create(cfg)
 
     def close(self):

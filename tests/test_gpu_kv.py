@@ -50,6 +50,20 @@ def test_attend_long_rows_are_split_and_joined(io, cache):
         c.check(got, r)
 
 
+@pytest.mark.parametrize("io,cache", [("bf16", "fp8"), ("f32", "f32")])
+def test_attend_many_short_rows_beside_long_ones(io, cache):
+    """More rows than blocks; the blocks' parts begin and end at any point of a row."""
+    rng = random.Random(3)
+    lens = [rng.choice([0, 1, 5, 16, 40, 90, 150]) for _ in range(700)]
+    lens[13], lens[400], lens[699] = 9000, 3000, 1
+    c = Cache(lens, H=2, G=2, D=64, page=16, io=io, cache=cache, seed=6)
+    got = c.attend()
+    for r in list(range(0, 700, 9)) + [13, 400, 699]:
+        c.check(got, r)
+    again = c.attend()
+    assert torch.equal(got[0].float(), again[0].float()) and torch.equal(got[1], again[1])
+
+
 @pytest.mark.parametrize("page", [16, 32, 256])
 @pytest.mark.parametrize("window", [1, 16, 31, 100, 1000])
 def test_attend_window(page, window):
@@ -422,6 +436,27 @@ def test_select_many_heads_in_a_group_and_long_tables():
     c = Cache([40, 20000 * 16 + 3], H=1, G=4, D=64, page=16, io="bf16", cache="fp8", seed=8, poison=False,
               max_pages=32768)
     run_select(c, 1000, 1, 2)
+
+
+@pytest.mark.parametrize("lens", [[601], [1999, 512, 513, 1], [2048, 2047], [4099, 77, 260]])
+def test_select_shared_by_several_blocks(lens):
+    """Few rows and wide tables: parts of odd sizes, parts without pages; twice, since
+    each call has to leave the counters as it found them."""
+    c = Cache([16 * n - 5 for n in lens], H=2, G=4, D=64, page=16, io="bf16", cache="fp8", seed=len(lens), poison=False,
+              max_pages=max(4200, max(lens)))
+    for keep in (3, 64, 250, 599):
+        run_select(c, keep, 1, 2)
+
+
+def test_select_without_a_workspace_or_with_owners_listed_twice():
+    c = Cache([16 * 900 - 5, 16 * 300], H=1, G=4, D=64, page=16, io="bf16", cache="fp8", seed=3, poison=False,
+              max_pages=2000)
+    first = run_select(c, 64, 1, 2)
+    assert torch.equal(first, run_select(c, 64, 1, 2, rows=i32([0, 1, 1, 0, 0])))
+    c.no_workspace = True
+    c.close()
+    c.kv = c.handle()
+    assert torch.equal(first, run_select(c, 64, 1, 2))
 
 
 def test_select_touches_the_listed_owners_only():

@@ -84,10 +84,13 @@ def test_create_refuses_reserved_and_small_workspace():
         config(k=A[2:3])
 
 
-def test_workspace_follows_the_head_layout_alone():
+def test_workspace_follows_the_head_layout_and_the_table():
     a = KV.rwttt_kv_workspace_bytes(config())
-    assert a == KV.rwttt_kv_workspace_bytes(config(n_owners=4096, max_pages=4000, n_pages=10 ** 6))
+    assert a == KV.rwttt_kv_workspace_bytes(config(n_pages=10 ** 6))
     assert a < KV.rwttt_kv_workspace_bytes(config(head_dim=256))
+    # at most 256 rows of scores, whatever the number of owners
+    b = KV.rwttt_kv_workspace_bytes(config(n_owners=4096, max_pages=4000))
+    assert b == KV.rwttt_kv_workspace_bytes(config(n_owners=128, max_pages=4000)) <= a + 256 * 4000 * 4 + 256
 
 
 EXTEND = dict(have=A[10], want=A[11], pos=A[12], new_pos=A[13], lengths=A[14], start=A[15], slots=A[16], owners=A[17],
