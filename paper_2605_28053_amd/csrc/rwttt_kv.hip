@@ -75,6 +75,7 @@ __device__ __forceinline__ int owner_of(const int* sums, int n, int i) {
   return lo;
 }
 
+template <int TURNS>
 __global__ void __launch_bounds__(kExtThreads) kv_extend_kernel(const KvExtendLaunch p) {
   extern __shared__ int ext_lds[];
   const int n = p.s.n_owners, shift = p.s.page_shift, P = 1 << shift;
@@ -82,70 +83,85 @@ __global__ void __launch_bounds__(kExtThreads) kv_extend_kernel(const KvExtendLa
   int* take = ext_lds;
   int* give = take + n + 1;
   int* add = give + n + 1;
-  __shared__ long long wave_sum[kExtThreads / 64][3];
+  __shared__ uint32_t wave_sum[kExtThreads / 64][4];
   __shared__ int any_bad;
   if (tid == 0) any_bad = 0;
   __syncthreads();
 
+  // four owners a thread and turn, their lengths kept for the second pass
   const int limit = p.s.max_pages << shift;
-  const int per = (n + kExtThreads - 1) / kExtThreads, i0 = min(n, tid * per), i1 = min(n, i0 + per);
-  long long t = 0, g = 0, a = 0;
+  const int turns = (n + 4 * kExtThreads - 1) / (4 * kExtThreads), i0 = tid * 4 * turns;
+  int have[TURNS * 4], want[TURNS * 4];
+#pragma unroll
+  for (int k = 0; k < TURNS; ++k) {
+    const int at = i0 + 4 * k;
+    const bool on = k < turns;
+    if (on && at + 4 <= n) {
+      const int4 h = *reinterpret_cast<const int4*>(p.have + at), w = *reinterpret_cast<const int4*>(p.want + at);
+      have[4 * k] = h.x, have[4 * k + 1] = h.y, have[4 * k + 2] = h.z, have[4 * k + 3] = h.w;
+      want[4 * k] = w.x, want[4 * k + 1] = w.y, want[4 * k + 2] = w.z, want[4 * k + 3] = w.w;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bool there = on && at + j < n;
+        have[4 * k + j] = there ? p.have[at + j] : 0;
+        want[4 * k + j] = there ? p.want[at + j] : 0;
+      }
+    }
+  }
+  const int front = p.pos[0], count = p.pos[1], pages = p.s.n_pages;
+  uint32_t t = 0, g = 0, a = 0;          // of a thread: 16 owners of 2^23 rows at most
   int bad = 0;
-  for (int i = i0; i < i1; ++i) {
-    int h = p.have[i], w = p.want[i];
-    bad |= h < 0 || w < 0 || h > limit || w > limit;
-    h = clampi(h, 0, limit);
-    w = clampi(w, 0, limit);
+#pragma unroll
+  for (int k = 0; k < TURNS * 4; ++k) {
+    bad |= have[k] < 0 || want[k] < 0 || have[k] > limit || want[k] > limit;
+    const int h = clampi(have[k], 0, limit), w = clampi(want[k], 0, limit);
     const int ph = (h + P - 1) >> shift, pw = (w + P - 1) >> shift;
     t += max(0, pw - ph);
     g += max(0, ph - pw);
     a += max(0, w - h);
   }
-  // exclusive sums over the threads, in 64 bits: the totals decide whether the step fits
-  long long st = t, sg = g, sa = a;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const long long x = __shfl_up(st, d), y = __shfl_up(sg, d), z = __shfl_up(sa, d);
-    if (lane >= d) {
-      st += x;
-      sg += y;
-      sa += z;
-    }
-  }
+  // Exclusive sums over the threads.  4096 owners have 2^31 pages at most; their new
+  // rows pass 32 bits, so the low 16 bits and the rest are summed apart.
+  const uint32_t st = wave_scan(t), sg = wave_scan(g), lo = wave_scan(a & 0xffffu), hi = wave_scan(a >> 16);
   if (lane == 63) {
     wave_sum[wave][0] = st;
     wave_sum[wave][1] = sg;
-    wave_sum[wave][2] = sa;
+    wave_sum[wave][2] = lo;
+    wave_sum[wave][3] = hi;
   }
   if (bad) any_bad = 1;
   __syncthreads();
-  long long bt = st - t, bg = sg - g, ba = sa - a, taken = 0, given = 0, added = 0;
+  long long bt = st - t, bg = sg - g, ba = (long long)lo + ((long long)hi << 16) - a, taken = 0, given = 0, added = 0;
+#pragma unroll
   for (int w = 0; w < kExtThreads / 64; ++w) {
+    const long long x = wave_sum[w][0], y = wave_sum[w][1], z = wave_sum[w][2] + ((long long)wave_sum[w][3] << 16);
     if (w < wave) {
-      bt += wave_sum[w][0];
-      bg += wave_sum[w][1];
-      ba += wave_sum[w][2];
+      bt += x;
+      bg += y;
+      ba += z;
     }
-    taken += wave_sum[w][0];
-    given += wave_sum[w][1];
-    added += wave_sum[w][2];
+    taken += x;
+    given += y;
+    added += z;
   }
-  const int front = p.pos[0], count = p.pos[1], pages = p.s.n_pages;
   int code = RWTTT_OK;
   if (any_bad || front < 0 || front >= pages || count < 0 || count > pages) code = RWTTT_E_INVALID;
   else if (taken > count || added > p.cap) code = RWTTT_E_CAPACITY;
   else if (count - taken + given > pages) code = RWTTT_E_INVALID;   // more pages than there are
   const bool ok = code == RWTTT_OK;
   if (ok) {
-    for (int i = i0; i < i1; ++i) {
-      const int h = p.have[i], w = p.want[i];
-      const int ph = (h + P - 1) >> shift, pw = (w + P - 1) >> shift;
-      take[i] = int(bt);
-      give[i] = int(bg);
-      add[i] = int(ba);
+#pragma unroll
+    for (int k = 0; k < TURNS * 4; ++k) {
+      const int ph = (have[k] + P - 1) >> shift, pw = (want[k] + P - 1) >> shift;
+      if (k < turns * 4 && i0 + k < n) {
+        take[i0 + k] = int(bt);
+        give[i0 + k] = int(bg);
+        add[i0 + k] = int(ba);
+      }
       bt += max(0, pw - ph);
       bg += max(0, ph - pw);
-      ba += max(0, w - h);
+      ba += max(0, want[k] - have[k]);
     }
     if (tid == 0) {
       take[n] = int(taken);
@@ -719,15 +735,16 @@ constexpr int kAttThreads = 256;
 
 struct AttendParams {
   KvAttendLaunch L;
-  uint32_t* count;       // [blocks]: partial results of the row that begins in a block, zero between calls
-  float* part;           // [blocks * 2][heads][D]
-  float* part_ml;        // [blocks * 2][heads][2]: maximum (of log2), sum
+  uint32_t* count;       // [blocks], then [windows * 2]: results that have been left, zero between calls
+  float* part;           // [blocks * 2 + windows * 2][heads][D]
+  float* part_ml;        // the same of [2]: maximum (of log2), sum
   int blocks, head_tiles, part_heads, acc_words;
   float scale_log2;      // scale * log2(e)
   bool stream;           // the cache passes through: non-temporal loads
 };
 
 constexpr int kAttWaves = kAttThreads / 64;
+constexpr int kJoinWindow = 32, kJoinDirect = 48;   // blocks of a row that are joined at once
 constexpr int kAttPad = 4;               // floats behind a query's sums in LDS: neighbours in other banks
 
 // Rows of keys a wave takes at a time.
@@ -820,10 +837,19 @@ struct Cut {
   }
 };
 
-// A part holds a short row, or a tile for each wave of a long one.
-constexpr int kPartCost = kRowCost + 4;
+// Smallest part of the line: a short row, or a few tiles of a long one.
+constexpr int kPartCost = 8;
 __device__ __forceinline__ int parts_of(uint64_t total, int blocks) {
   return total >= uint64_t(blocks) * kPartCost ? blocks : int(uint32_t(total + kPartCost - 1) / kPartCost);
+}
+
+// A cut that falls in a short row, or near an end of a long one, moves to the
+// row's end: joining costs more than the imbalance.
+constexpr uint32_t kShortRow = kRowCost + 12, kRowHead = kRowCost + 3, kRowTail = 3;
+static_assert(kShortRow > kRowHead + kRowTail, "a row that is split keeps a middle");
+__device__ __forceinline__ uint32_t snapped(uint32_t x, uint32_t cost) {
+  if (cost <= kShortRow || x <= kRowHead) return 0;
+  return x >= cost - kRowTail ? cost : x;
 }
 
 template <int W, bool HINT = false> __device__ __forceinline__ void load_words(const char* p, uint32_t* w) {
@@ -933,34 +959,41 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
   const int parts = parts_of(total, ap.blocks), b = blockIdx.x;
   if (b >= parts) return;
   const Cut cut(total, parts);
-  uint64_t u = cut.begin(b);
-  const uint64_t end = cut.begin(b + 1);
-
   int i = 0;                             // the listed owner that u lies in
-  for (int hi = n; hi - i > 1;) {
-    const int mid = (i + hi) >> 1;
-    if (uint64_t(pre[mid]) * VH <= u) i = mid;
-    else hi = mid;
+  uint64_t u = total, end = total;       // the block's part, its cuts where they are made
+#pragma unroll 1
+  for (int k = 1; k >= 0; --k) {
+    end = u;
+    u = cut.begin(b + k);
+    if (u >= total) continue;            // behind the last part
+    i = 0;
+    for (int hi = n; hi - i > 1;) {
+      const int mid = (i + hi) >> 1;
+      if (uint64_t(pre[mid]) * VH <= u) i = mid;
+      else hi = mid;
+    }
+    const uint32_t cost = pre[i + 1] - pre[i];
+    const uint32_t x = uint32_t(u - uint64_t(pre[i]) * VH) % cost;   // an owner's tiles and heads fit 32 bits
+    u += uint64_t(snapped(x, cost)) - x;
   }
   i = __builtin_amdgcn_readfirstlane(i);
 
   while (u < end) {
     const uint32_t cost = __builtin_amdgcn_readfirstlane(pre[i + 1] - pre[i]);
-    if (cost == 0) {
+    const uint32_t x = uint32_t(u - uint64_t(pre[i]) * VH);
+    const int vh = __builtin_amdgcn_readfirstlane(int(x / max(cost, 1u)));
+    if (cost == 0 || vh == VH) {         // no rows, or the cut moved to the owner's end
       ++i;
       continue;
     }
     const int tiles = int(cost) - kRowCost;
-    const uint32_t x = uint32_t(u - uint64_t(pre[i]) * VH);    // an owner's tiles and heads fit 32 bits
-    const int vh = __builtin_amdgcn_readfirstlane(int(x / cost));
     const uint32_t x0 = __builtin_amdgcn_readfirstlane(x % cost);
     const uint32_t x1 = uint32_t(min(uint64_t(cost), x0 + (end - u)));
     const int seg0 = max(0, int(x0) - kRowCost), seg1 = max(0, int(x1) - kRowCost);
-    const uint64_t u0 = u - x0 + kRowCost;                     // the row's first tile in the line
+    const uint64_t u0 = u - x0;          // the row's place in the line
     u += x1 - x0;
     const int at_row = i;
     if (x1 == cost && vh == VH - 1) ++i;
-    if (seg0 == seg1) continue;
     const int t0 = seg0 + int(uint32_t(seg1 - seg0) * wave / kAttWaves);
     const int t1 = seg0 + int(uint32_t(seg1 - seg0) * (wave + 1) / kAttWaves);
     const int owner = __builtin_amdgcn_readfirstlane(rt.owner[at_row]);
@@ -993,41 +1026,16 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
       return at;
     };
 
-    // queries: the lane's column is one of them
-    const size_t q_at = size_t(owner) * p.q_stride + (size_t(h) * G + head0 + (c < heads ? c : 0)) * D;
-    bf16x8_t q[F ? 1 : NQ][F ? 1 : D / 32];
-    f32x4_t qf[F ? D / 16 : 1];
-    if constexpr (F) {
+    // queries: the lane's column is one of them; piece s of its channels feeds PER operands
+    constexpr int PER = F ? 1 : S::KE / 8, QN = F ? D / 16 : D / 32, QW = F || IO ? 4 : 8;
+    const char* q_at = static_cast<const char*>(p.q) +
+                       (size_t(owner) * p.q_stride + (size_t(h) * G + head0 + (c < heads ? c : 0)) * D) * (IO ? 2 : 4);
+    uint32_t qw[QN][QW];
 #pragma unroll
-      for (int s = 0; s < D / 16; ++s) {
-        const float* src = static_cast<const float*>(p.q) + q_at + S::key_channel(s, g);
-        qf[s] = *reinterpret_cast<const f32x4_t*>(src);
-        if (c >= heads) qf[s] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-      }
-    } else {
+    for (int s = 0; s < QN; ++s) {
+      const int ch = S::key_channel(s / PER, g) + (s % PER) * 8;
 #pragma unroll
-      for (int s = 0; s < D / 32; ++s) {
-        constexpr int PER = S::KE / 8;                  // operands a piece of keys feeds
-        const int ch = S::key_channel(s / PER, g) + (s % PER) * 8;
-        if constexpr (IO) {
-          uint32_t wd[4];
-          load_words<4>(static_cast<const char*>(p.q) + (q_at + ch) * 2, wd);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) wd[j] = c < heads ? wd[j] : 0u;
-          q[0][s] = as_bf16x8(wd);
-        } else {
-          float f[8];
-          uint32_t wd[8];
-          load_words<4>(static_cast<const char*>(p.q) + (q_at + ch) * 4, wd);
-          load_words<4>(static_cast<const char*>(p.q) + (q_at + ch) * 4 + 16, wd + 4);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) f[j] = c < heads ? __uint_as_float(wd[j]) : 0.f;
-          bf16x8_t terms[NQ];
-          split_bf16<NQ>(f, terms);
-#pragma unroll
-          for (int k = 0; k < NQ; ++k) q[k][s] = terms[k];
-        }
-      }
+      for (int j = 0; j < QW; j += 4) load_words<4>(q_at + ch * (IO ? 2 : 4) + j * 4, &qw[s][j]);
     }
     const float to_log2 = ap.scale_log2 * (CT == RWTTT_FP8 && p.k_scale ? p.k_scale[h] : 1.f);
 
@@ -1066,9 +1074,34 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
     };
 
     TileAt<NT> at = locate(min(t0, seg1 - 1)), next = at;
-    if (t0 < t1) {
+    // With the condition the compiler keeps a second set of registers and loads the
+    // next tile while this one is in use: 347 against 373 us for 16 owners of 8500
+    // rows, head dim 256, fp32.  Three terms of a query leave no room for it.
+    constexpr bool kSecondSet = IO || CT != RWTTT_BF16;
+    if (!kSecondSet || t0 < t1) {
       load_keys(at);
       load_values(at);
+    }
+    bf16x8_t q[F ? 1 : NQ][F ? 1 : QN];
+    f32x4_t qf[F ? QN : 1];
+#pragma unroll
+    for (int s = 0; s < QN; ++s) {
+#pragma unroll
+      for (int j = 0; j < QW; ++j) qw[s][j] = c < heads ? qw[s][j] : 0u;
+      if constexpr (F) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) qf[s][j] = __uint_as_float(qw[s][j]);
+      } else if constexpr (IO) {
+        q[0][s] = as_bf16x8(qw[s]);
+      } else {
+        float f[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(qw[s][j]);
+        bf16x8_t terms[NQ];
+        split_bf16<NQ>(f, terms);
+#pragma unroll
+        for (int k = 0; k < NQ; ++k) q[k][s] = terms[k];
+      }
     }
     for (int t = t0; t < t1; ++t) {
       const bool more = t + 1 < t1;
@@ -1187,30 +1220,23 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
 
-    // the waves' sums, each relative to the block's maximum, into LDS:
-    // acc[e * VE + a][j] is channel value_channel(e, 4 g + j) + a of query c
+    // the waves' sums into LDS: acc[e * VE + a][j] is channel
+    // value_channel(e, 4 g + j) + a of query c
     constexpr int DP = D + kAttPad;
     if (g == 0) {
       wave_ml[wave][c][0] = m;
       wave_ml[wave][c][1] = l;
     }
-    __syncthreads();
-    {
-      float top = wave_ml[0][c][0];
+    if (c < heads) {
 #pragma unroll
-      for (int k = 1; k < kAttWaves; ++k) top = fmaxf(top, wave_ml[k][c][0]);
-      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-      if (c < heads) {
+      for (int e = 0; e < S::NE; ++e)
 #pragma unroll
-        for (int e = 0; e < S::NE; ++e)
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int a = 0; a < S::VE; a += 4)
-              *reinterpret_cast<f32x4_t*>(wave_acc + (wave * heads + c) * DP + S::value_channel(e, g * 4 + j) + a) =
-                  (f32x4_t){acc[e * S::VE + a][j] * f, acc[e * S::VE + a + 1][j] * f,
-                            acc[e * S::VE + a + 2][j] * f, acc[e * S::VE + a + 3][j] * f};
-      }
+          for (int a = 0; a < S::VE; a += 4)
+            *reinterpret_cast<f32x4_t*>(wave_acc + (wave * heads + c) * DP + S::value_channel(e, g * 4 + j) + a) =
+                (f32x4_t){acc[e * S::VE + a][j], acc[e * S::VE + a + 1][j], acc[e * S::VE + a + 2][j],
+                          acc[e * S::VE + a + 3][j]};
     }
     __syncthreads();
 
@@ -1229,6 +1255,11 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
         p.lse[(size_t(owner) * H + h) * G + head0 + head] =
             total_l == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total_l)) * 0.6931471805599453f;
     };
+    auto leave = [&](size_t slot, int col, f32x4_t sum, float top, float total_l) {
+      share(ap.part + slot * D + col * 4, sum[0], sum[1]);
+      share(ap.part + slot * D + col * 4 + 2, sum[2], sum[3]);
+      if (col == 0) share(ap.part_ml + slot * 2, top, total_l);
+    };
     const bool complete = seg0 == 0 && seg1 == tiles;
     for (int k = tid; k < cols; k += kAttThreads) {
       const int head = k / LPR, col = k % LPR;
@@ -1238,71 +1269,72 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
       for (int v = 0; v < kAttWaves; ++v) top = fmaxf(top, wave_ml[v][head][0]);
 #pragma unroll
       for (int v = 0; v < kAttWaves; ++v) {
-        sum += *reinterpret_cast<const f32x4_t*>(wave_acc + (v * heads + head) * DP + col * 4);
-        const float mv = wave_ml[v][head][0];
-        sl += (mv == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mv - top)) * wave_ml[v][head][1];
+        const float mv = wave_ml[v][head][0], f = mv == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mv - top);
+        sum += f * *reinterpret_cast<const f32x4_t*>(wave_acc + (v * heads + head) * DP + col * 4);
+        sl += f * wave_ml[v][head][1];
       }
       if (complete) {
         write_out(head, col, sum, top, sl);
       } else {
-        const size_t slot = (size_t(b) * 2 + (seg0 == 0 ? 1 : 0)) * ap.part_heads + head;
-        share(ap.part + slot * D + col * 4, sum[0], sum[1]);
-        share(ap.part + slot * D + col * 4 + 2, sum[2], sum[3]);
-        if (col == 0) share(ap.part_ml + slot * 2, top, sl);
+        leave((size_t(b) * 2 + (seg0 == 0 ? 1 : 0)) * ap.part_heads + head, col, sum, top, sl);
       }
     }
     if (!complete) {
-      // the row's blocks are neighbours; the first one's counter is the row's, since
-      // only the last row of a block's part can go on behind it
-      const int b0 = cut.part_of(u0), b1 = cut.part_of(u0 + tiles - 1);
-      shared_done();
-      __syncthreads();
-      if (tid == 0) {
-        arrived = atomicAdd(&ap.count[b0], 1u);
-        if (arrived == uint32_t(b1 - b0)) ap.count[b0] = 0;
-      }
-      __syncthreads();
-      if (arrived == uint32_t(b1 - b0)) {
+      // The row's blocks are neighbours.  A few are joined at once; more in windows
+      // of 32 neighbours first, then the windows.  Counters: of the row, the one of
+      // its first block, since only the last row of a block's part can go on behind
+      // it; of a window, one for the row that began before it and one for the row
+      // that begins in it and goes on.
+      const int b0 = cut.part_of(u0 + kRowHead), b1 = cut.part_of(u0 + cost - kRowTail - 1);
+      const int w = b / kJoinWindow, w0 = b0 / kJoinWindow, w1 = b1 / kJoinWindow;
+      bool final = b1 - b0 < kJoinDirect;
+      int k0 = final ? b0 : max(b0, w * kJoinWindow), k1 = final ? b1 : min(b1, (w + 1) * kJoinWindow - 1);
+      uint32_t* count = final ? &ap.count[b0] : &ap.count[ap.blocks + w * 2 + (w == w0 ? 1 : 0)];
+      int slots = 0, first = b0;         // result k is in slot slots + 2 k + (k == first)
+#pragma unroll 1
+      for (;;) {
+        // the block that finds all others counted goes on
+        shared_done();
+        __syncthreads();
+        if (tid == 0) {
+          arrived = atomicAdd(count, 1u);
+          if (arrived == uint32_t(k1 - k0)) *count = 0;
+        }
+        __syncthreads();
+        if (arrived != uint32_t(k1 - k0)) break;
         const int groups = max(1, kAttThreads / cols);
         float* merge = wave_acc;         // [groups][cols][6] where there is more than one group
-        for (int k0 = 0; k0 < cols; k0 += kAttThreads) {
-          const int k = groups > 1 ? tid % cols : k0 + tid, part = groups > 1 ? tid / cols : 0;
+        for (int c0 = 0; c0 < cols; c0 += kAttThreads) {
+          const int k = groups > 1 ? tid % cols : c0 + tid, part = groups > 1 ? tid / cols : 0;
           const bool on = k < cols && part < groups;
           const int head = k / LPR, col = k % LPR;
           f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
           float top = -INFINITY, sl = 0.f;
+          auto add = [&](float xm, float xl, f32x4_t x) {
+            const float up = fmaxf(top, xm), ref = up == -INFINITY ? 0.f : up;
+            const float f = __builtin_amdgcn_exp2f(top - ref), fx = __builtin_amdgcn_exp2f(xm - ref);
+            sum = f * sum + fx * x;
+            sl = f * sl + fx * xl;
+            top = up;
+          };
           if (on) {
-            constexpr int U = 8;         // partial results in flight
-            for (int w = b0 + part; w <= b1; w += U * groups) {
+            constexpr int U = 8;         // results in flight
+#pragma unroll 1
+            for (int s = k0 + part; s <= k1; s += U * groups) {
               f32x4_t x[U];
-              float xm[U], xl[U];
+              float2 ml[U];
 #pragma unroll
               for (int v = 0; v < U; ++v) {
-                const int at_b = min(w + v * groups, b1);
-                const size_t slot = (size_t(at_b) * 2 + (at_b == b0 ? 1 : 0)) * ap.part_heads + head;
-                const float2 lo = shared_pair(ap.part + slot * D + col * 4);
-                const float2 hi = shared_pair(ap.part + slot * D + col * 4 + 2);
-                const float2 ml = shared_pair(ap.part_ml + slot * 2);
+                const int r = min(s + v * groups, k1);
+                const size_t at_r = size_t(slots + 2 * r + (r == first ? 1 : 0)) * ap.part_heads + head;
+                const float2 lo = shared_pair(ap.part + at_r * D + col * 4);
+                const float2 hi = shared_pair(ap.part + at_r * D + col * 4 + 2);
+                ml[v] = shared_pair(ap.part_ml + at_r * 2);
                 x[v] = (f32x4_t){lo.x, lo.y, hi.x, hi.y};
-                xm[v] = ml.x;
-                xl[v] = ml.y;
               }
-              float up = top;
 #pragma unroll
               for (int v = 0; v < U; ++v)
-                if (w + v * groups <= b1) up = fmaxf(up, xm[v]);
-              const float ref = up == -INFINITY ? 0.f : up;
-              const float f = __builtin_amdgcn_exp2f(top - ref);
-              sum *= f;
-              sl *= f;
-              top = up;
-#pragma unroll
-              for (int v = 0; v < U; ++v)
-                if (w + v * groups <= b1) {
-                  const float fv = __builtin_amdgcn_exp2f(xm[v] - ref);
-                  sum += fv * x[v];
-                  sl += fv * xl[v];
-                }
+                if (s + v * groups <= k1) add(ml[v].x, ml[v].y, x[v]);
             }
           }
           if (groups > 1) {
@@ -1314,25 +1346,24 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
               for (int d = 0; d < 4; ++d) at_m[2 + d] = sum[d];
             }
             __syncthreads();
-            if (on && part == 0) {
-              float up = top;
-              for (int v = 1; v < groups; ++v) up = fmaxf(up, merge[size_t(v * cols + k) * 6]);
-              const float ref = up == -INFINITY ? 0.f : up;
-              const float f = __builtin_amdgcn_exp2f(top - ref);
-              sum *= f;
-              sl *= f;
+            if (on && part == 0)
               for (int v = 1; v < groups; ++v) {
                 const float* at_m = merge + size_t(v * cols + k) * 6;
-                const float fv = __builtin_amdgcn_exp2f(at_m[0] - ref);
-                sl += fv * at_m[1];
-#pragma unroll
-                for (int d = 0; d < 4; ++d) sum[d] += fv * at_m[2 + d];
+                add(at_m[0], at_m[1], (f32x4_t){at_m[2], at_m[3], at_m[4], at_m[5]});
               }
-              top = up;
-            }
           }
-          if (on && part == 0) write_out(head, col, sum, top, sl);
+          if (on && part == 0) {
+            if (final) write_out(head, col, sum, top, sl);
+            else leave(size_t(ap.blocks * 2 + w * 2 + (w == w0 ? 1 : 0)) * ap.part_heads + head, col, sum, top, sl);
+          }
         }
+        if (final) break;
+        final = true;
+        k0 = w0;
+        k1 = w1;
+        count = &ap.count[b0];
+        slots = ap.blocks * 2;
+        first = w0;
       }
     }
     __syncthreads();                     // the next row's sums go to the same LDS
@@ -1364,9 +1395,10 @@ struct KvWorkspace {
       used += (n + 255) / 256 * 256;
       return q;
     };
-    const size_t slots = size_t(kAttBlocks) * 2 * part_heads_of(s.group);
+    const size_t windows = kAttBlocks / kJoinWindow * 2;
+    const size_t slots = (size_t(kAttBlocks) * 2 + windows) * part_heads_of(s.group);
     const size_t rows = select_rows(s);
-    attend_count = reinterpret_cast<uint32_t*>(take(kAttBlocks * sizeof(uint32_t)));
+    attend_count = reinterpret_cast<uint32_t*>(take((kAttBlocks + windows) * sizeof(uint32_t)));
     select_count = reinterpret_cast<uint32_t*>(take(kSelRows * sizeof(uint32_t)));
     part = reinterpret_cast<float*>(take(slots * s.head_dim * sizeof(float)));
     part_ml = reinterpret_cast<float*>(take(slots * 2 * sizeof(float)));
@@ -1382,8 +1414,10 @@ size_t kv_workspace_bytes(const KvShape& shape) { return KvWorkspace(nullptr, sh
 hipError_t launch_kv_extend(const KvExtendLaunch& L, hipStream_t stream) {
   const unsigned blocks = (L.cap + kExtItems - 1) / kExtItems;
   const size_t lds = size_t(L.s.n_owners + 1) * 3 * sizeof(int);
-  hipLaunchKernelGGL(kv_extend_kernel, dim3(blocks < 1 ? 1 : blocks > 512 ? 512 : blocks), dim3(kExtThreads), lds,
-                     stream, L);
+  const dim3 grid(blocks < 1 ? 1 : blocks > 512 ? 512 : blocks), block(kExtThreads);
+  // sixteen owners' lengths in a thread's registers cost the small calls 2 us
+  if (L.s.n_owners <= 4 * kExtThreads) hipLaunchKernelGGL(kv_extend_kernel<1>, grid, block, lds, stream, L);
+  else hipLaunchKernelGGL(kv_extend_kernel<RWTTT_KV_MAX_OWNERS / (4 * kExtThreads)>, grid, block, lds, stream, L);
   return hipGetLastError();
 }
 
@@ -1482,7 +1516,7 @@ hipError_t launch_kv_select(const KvSelectLaunch& L, hipStream_t stream) {
 hipError_t launch_kv_attend(const KvAttendLaunch& L, hipStream_t stream) {
   AttendParams p;
   p.L = L;
-  p.blocks = kAttBlocks;
+  p.blocks = L.s.head_dim == 256 ? kAttBlocks / 2 : kAttBlocks;   // what is resident at once: one or two a CU
   p.head_tiles = (L.s.group + 15) / 16;
   p.part_heads = part_heads_of(L.s.group);
   const KvWorkspace ws(L.workspace, L.s);
