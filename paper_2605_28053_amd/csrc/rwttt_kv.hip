@@ -1318,7 +1318,7 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
             top = up;
           };
           if (on) {
-            constexpr int U = 8;         // results in flight
+            constexpr int U = 4;         // results in flight
 #pragma unroll 1
             for (int s = k0 + part; s <= k1; s += U * groups) {
               f32x4_t x[U];
