@@ -966,12 +966,11 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
     end = u;
     u = cut.begin(b + k);
     if (u >= total) continue;            // behind the last part
-    i = 0;
-    for (int hi = n; hi - i > 1;) {
-      const int mid = (i + hi) >> 1;
-      if (uint64_t(pre[mid]) * VH <= u) i = mid;
-      else hi = mid;
-    }
+    // 64 owners at a look
+    const int stride = (n + 63) / 64;
+    i = (__builtin_popcountll(__ballot(lane * stride < n && uint64_t(pre[min(lane * stride, n)]) * VH <= u)) - 1) * stride;
+    if (stride > 1)
+      i += __builtin_popcountll(__ballot(lane < stride && i + lane < n && uint64_t(pre[min(i + lane, n)]) * VH <= u)) - 1;
     const uint32_t cost = pre[i + 1] - pre[i];
     const uint32_t x = uint32_t(u - uint64_t(pre[i]) * VH) % cost;   // an owner's tiles and heads fit 32 bits
     u += uint64_t(snapped(x, cost)) - x;
