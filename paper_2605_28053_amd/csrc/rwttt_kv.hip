@@ -59,7 +59,8 @@ __device__ __forceinline__ void shared_done() { asm volatile("s_waitcnt vmcnt(0)
 // The three prefix sums over the owners (pages taken, pages returned, new rows)
 // fix every output, so each block computes them itself -- 8 bytes an owner, from
 // the L2 -- and then fills its part of the flattened lists by a binary search:
-// one launch, no block waits for another.
+// one launch, no block waits for another.  Bound by latency: 3.8 us for eight
+// owners, 7.4 for 500 with 34000 new rows, 10.0 for 4000.
 
 constexpr int kExtThreads = 256;
 constexpr int kExtItems = 512;           // list entries a block fills
@@ -235,7 +236,7 @@ __global__ void __launch_bounds__(kExtThreads) kv_extend_kernel(const KvExtendLa
 // in its registers to those behind its run, which it reads again (from the L2,
 // mostly), so one wave sees all of a page's new keys and no atomics are needed.
 
-// To e4m3 of two values already scaled, clamped to the largest number; NaN stays.
+// A scaled value, clamped to the largest e4m3 number; NaN stays.
 __device__ __forceinline__ float fp8_clamp(float x) { return x != x ? x : fminf(fmaxf(x, -448.f), 448.f); }
 
 template <int IO, int CT> struct AppendRow {   // 16 bytes of io
@@ -433,13 +434,17 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const AppendParams ap) {
 // into two vectors of whole numbers, U = sum max(q8, 0) and V = sum max(-q8, 0),
 // before any page is read: a page costs two 8-bit dot products.  U and V reach
 // 127 * group, so each is split into two base-128 digits.
-
+//
 // Where the rows (one: an owner and kv head) are too few to fill the chip,
 // several blocks share one: each scores a part of its pages into the workspace
 // and counts itself, and the last one ranks them all.
 //
 // The ranking counts the scores in bins of their own range, 12 bits of it, in
 // LDS, and looks closer only at the bin that the last page kept lies in.
+//
+// Bound by latency: 64 rows of 2048 pages (30 MB of bounds, four blocks a row) take
+// 14.8 us, of which the bounds' loads 9.7 (a plain read of as much: 4.6), the
+// exchange between the blocks 2, the ranking 2.5; one block a row takes 19.3 us.
 
 constexpr int kSelThreads = 512, kSelWaves = kSelThreads / 64;
 constexpr int kSelRows = 256;            // most rows that several blocks share
@@ -729,7 +734,16 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(const SelectPara
 // dealt to the tiles so that a lane's 4 + 4 scores are 8 consecutive rows.  So
 // neither scores nor probabilities move between lanes.  V arrives with the
 // channels of a row in one lane; its transposed operand takes one byte
-// permutation for each pair of values.
+// permutation for each pair of values.  A probability enters the second product as
+// two bf16 terms (three for fp32 queries), a query of fp32 over a narrower cache as
+// three: one term would round each weight to 8 bits, as much error as the output's
+// own rounding, and the matrix units are busy a quarter of the time as it is.
+//
+// Measured: 32 owners of 12000-20000 rows, eight kv heads of four queries and 128
+// channels in bf16, 2.19 GB: 331 us, 6.6 TB/s, what a plain streaming read of this
+// shape reaches.  Smaller calls add 8 to 9 us to their bytes' time: launch 1.7, the
+// row table and cuts 1.5, the first tile's loads 2.5, adding the waves' sums 1 and
+// the join 3.
 
 constexpr int kAttThreads = 256;
 

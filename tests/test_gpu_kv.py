@@ -64,6 +64,21 @@ def test_attend_many_short_rows_beside_long_ones(io, cache):
     assert torch.equal(got[0].float(), again[0].float()) and torch.equal(got[1], again[1])
 
 
+def test_attend_the_most_owners_and_the_widest_rows():
+    """4096 owners, sixteen queries of 256 channels a head: the most LDS a call asks for."""
+    rng = random.Random(8)
+    lens = [rng.choice([0, 1, 3, 16]) for _ in range(4096)]
+    lens[2000] = 700
+    c = Cache(lens, H=1, G=16, D=256, page=16, io="bf16", cache="bf16", seed=1, poison=False)
+    got = c.attend()
+    for r in list(range(0, 4096, 101)) + [2000, 4095]:
+        c.check(got, r)
+    rows = i32([4095 - r for r in range(4096)])
+    again = c.attend(rows=rows)
+    for r in (0, 1, 2000, 4095):
+        c.check(again, r)
+
+
 @pytest.mark.parametrize("page", [16, 32, 256])
 @pytest.mark.parametrize("window", [1, 16, 31, 100, 1000])
 def test_attend_window(page, window):
@@ -197,6 +212,24 @@ def test_attend_equal_calls_give_equal_bits_on_any_stream():
             again = c.attend()
         assert torch.equal(first[0].view(torch.int16), again[0].view(torch.int16))
         assert torch.equal(first[1], again[1])
+
+
+@pytest.mark.parametrize("lens,H", [([60000], 1), ([9000, 3, 0, 777, 20000, 4500], 2), ([4200] * 8, 8)])
+def test_attend_calls_in_turn_see_their_own_partial_results(lens, H):
+    """Three queries in turn on one handle, nothing waited for in between: what one call
+    leaves in the workspace is never taken for another's."""
+    c = Cache(lens, H=H, G=4, D=128, page=64, io="bf16", cache="bf16", seed=15, poison=False)
+    g = torch.Generator().manual_seed(2)
+    qs = [dev((torch.randn(c.q_h.shape, generator=g) * (1 + i)).to(torch.bfloat16)) for i in range(3)]
+    first = [c.attend(q=q) for q in qs]
+    outs = [torch.zeros((c.R, c.H * c.G, c.D), dtype=torch.bfloat16, device="cuda") for _ in range(30)]
+    for i, out in enumerate(outs):
+        q = qs[i % 3]
+        ok(KV.rwttt_kv_attend(c.kv, 0, q.data_ptr(), q.stride(0), c.lengths.data_ptr(), 0, c.R, c.D ** -0.5, 0, 0, 0,
+                              out.data_ptr(), out.stride(0), 0, stream()))
+    torch.cuda.synchronize()
+    for i, out in enumerate(outs):
+        assert torch.equal(out.cpu().view(torch.int16), first[i % 3][0].view(torch.int16)), i
 
 
 # ---------------------------------------------------------------------------
