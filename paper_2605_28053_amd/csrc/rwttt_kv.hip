@@ -758,7 +758,10 @@ struct AttendParams {
 };
 
 constexpr int kAttWaves = kAttThreads / 64;
-constexpr int kJoinWindow = 32, kJoinDirect = 48;   // blocks of a row that are joined at once
+// Blocks of a row that are joined at once; more go in windows first, since one block
+// reads all it joins: a row over all 512 blocks (131072 rows of one head) took 67 us
+// that way and takes 27.  The second level costs about 3 us, 48 results no more.
+constexpr int kJoinWindow = 32, kJoinDirect = 48;
 constexpr int kAttPad = 4;               // floats behind a query's sums in LDS: neighbours in other banks
 
 // Rows of keys a wave takes at a time.
@@ -851,14 +854,17 @@ struct Cut {
   }
 };
 
-// Smallest part of the line: a short row, or a few tiles of a long one.
+// Smallest part of the line: a short row, or a few tiles of a long one.  One owner
+// of 4224 rows takes 15.0, 13.5, 13.1 and 13.3 us with 4, 6, 8 and 12: smaller parts
+// have more results to join.
 constexpr int kPartCost = 8;
 __device__ __forceinline__ int parts_of(uint64_t total, int blocks) {
   return total >= uint64_t(blocks) * kPartCost ? blocks : int(uint32_t(total + kPartCost - 1) / kPartCost);
 }
 
 // A cut that falls in a short row, or near an end of a long one, moves to the
-// row's end: joining costs more than the imbalance.
+// row's end: joining costs more than the imbalance (64 owners of up to 300 rows 17.2
+// -> 13.4 us; 24 tiles as the bound of a short row measure the same).
 constexpr uint32_t kShortRow = kRowCost + 12, kRowHead = kRowCost + 3, kRowTail = 3;
 static_assert(kShortRow > kRowHead + kRowTail, "a row that is split keeps a middle");
 __device__ __forceinline__ uint32_t snapped(uint32_t x, uint32_t cost) {
@@ -1501,7 +1507,9 @@ hipError_t launch_kv_select(const KvSelectLaunch& L, hipStream_t stream) {
   const KvWorkspace ws(L.workspace, L.s);
   p.count = ws.select_count;
   p.score = ws.score;
-  // about two blocks a CU, each with enough pages to be worth the exchange
+  // Each part with enough pages to be worth the exchange, and about two blocks a CU:
+  // 64 rows of 2048 pages take 19.3, 16.1, 14.8 and 16.0 us in 1, 2, 4 and 8 parts, 66
+  // rows of 564 pages 8.1 and 8.6 us in 1 and 2.
   const int rows = int(L.n) * L.s.kv_heads;
   p.splits = 1;
   if (L.workspace && rows <= select_rows(L.s))
@@ -1529,7 +1537,10 @@ hipError_t launch_kv_select(const KvSelectLaunch& L, hipStream_t stream) {
 hipError_t launch_kv_attend(const KvAttendLaunch& L, hipStream_t stream) {
   AttendParams p;
   p.L = L;
-  p.blocks = L.s.head_dim == 256 ? kAttBlocks / 2 : kAttBlocks;   // what is resident at once: one or two a CU
+  // What is resident at once: two blocks a CU, one for 256 channels, whose registers
+  // leave room for no more (16 owners of 8500 rows: 180 us in bf16 and 94 in e4m3 so,
+  // 184 and 102 with twice the blocks).
+  p.blocks = L.s.head_dim == 256 ? kAttBlocks / 2 : kAttBlocks;
   p.head_tiles = (L.s.group + 15) / 16;
   p.part_heads = part_heads_of(L.s.group);
   const KvWorkspace ws(L.workspace, L.s);
