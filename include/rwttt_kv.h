@@ -150,7 +150,7 @@ rwttt_status rwttt_kv_append(rwttt_kv* kv, uint32_t layer, const void* k, uint64
  * them when it has no more than keep.  pages: [n_owners, n_kv_heads, keep],
  * positions in the owner's table row, ascending, -1 behind the last.
  * The score bounds what the page's keys can add to the logits of the head's
- * queries together.  With a the largest magnitude in the group's queries and
+ * (rounded) queries together.  With a the largest magnitude in the group's queries and
  * q8 = rint(q * ((1 / a) * 127)), each step rounded to fp32 (0 for a = 0, or so
  * small that 1 / a overflows),
  *     score = sum over the group's queries and channels of max(q8 lo, q8 hi):

@@ -49,6 +49,13 @@ __device__ __forceinline__ float2 shared_pair(const float* p) {
   const uint64_t w = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   return make_float2(__uint_as_float(uint32_t(w)), __uint_as_float(uint32_t(w >> 32)));
 }
+// Counts this block; true for the one that finds `others` counted, which leaves the
+// counter zero for the next call -- past the L2 too, whose line holds other counters.
+__device__ __forceinline__ uint32_t count_in(uint32_t* count, uint32_t others) {
+  const uint32_t before = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (before == others) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return before == others;
+}
 // The thread's shared stores have reached the memory that all XCDs see.
 __device__ __forceinline__ void shared_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
@@ -591,12 +598,9 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(const SelectPara
                          __HIP_MEMORY_SCOPE_AGENT);
     shared_done();
     __syncthreads();
-    if (tid == 0) {
-      pick[0] = atomicAdd(&sp.count[row], 1u);
-      if (pick[0] == uint32_t(sp.splits - 1)) sp.count[row] = 0;
-    }
+    if (tid == 0) pick[0] = count_in(&sp.count[row], uint32_t(sp.splits - 1));
     __syncthreads();
-    if (pick[0] != uint32_t(sp.splits - 1)) return;
+    if (!pick[0]) return;
     for (int k = tid; k < (np + 1) / 2; k += kSelThreads) {
       const uint64_t w = __hip_atomic_load(shared_key + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       key[2 * k] = uint32_t(w);
@@ -952,7 +956,7 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
   const KvAttendLaunch& p = ap.L;
   __shared__ uint32_t wave_sum[kAttWaves];
   __shared__ float wave_ml[kAttWaves][16][2];
-  __shared__ uint32_t arrived;
+  __shared__ uint32_t last;
   extern __shared__ float wave_acc[];    // [waves][heads][D + kAttPad], then the row table
   const RowTable rt(reinterpret_cast<uint32_t*>(wave_acc + ap.acc_words), int(p.n));
   const uint32_t* pre = rt.pre;
@@ -1315,12 +1319,9 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
         // the block that finds all others counted goes on
         shared_done();
         __syncthreads();
-        if (tid == 0) {
-          arrived = atomicAdd(count, 1u);
-          if (arrived == uint32_t(k1 - k0)) *count = 0;
-        }
+        if (tid == 0) last = count_in(count, uint32_t(k1 - k0));
         __syncthreads();
-        if (arrived != uint32_t(k1 - k0)) break;
+        if (!last) break;
         const int groups = max(1, kAttThreads / cols);
         float* merge = wave_acc;         // [groups][cols][6] where there is more than one group
         for (int c0 = 0; c0 < cols; c0 += kAttThreads) {
@@ -1431,7 +1432,12 @@ struct KvWorkspace {
 size_t kv_workspace_bytes(const KvShape& shape) { return KvWorkspace(nullptr, shape).bytes; }
 
 hipError_t launch_kv_extend(const KvExtendLaunch& L, hipStream_t stream) {
-  const unsigned blocks = (L.cap + kExtItems - 1) / kExtItems;
+  // two map entries a thread; and where the cache is large, blocks for the pages that
+  // ending owners may return with no new row beside them, 16 a thread if all do (128000
+  // pages of 64 owners: 12.5 us, 299 from one block; a decode step in that cache 8.5 us
+  // a call either way)
+  const unsigned maps = (L.cap + kExtItems - 1) / kExtItems, pages = (unsigned(L.s.n_pages) + 4095) / 4096;
+  const unsigned blocks = maps > pages ? maps : pages;
   const size_t lds = size_t(L.s.n_owners + 1) * 3 * sizeof(int);
   const dim3 grid(blocks < 1 ? 1 : blocks > 512 ? 512 : blocks), block(kExtThreads);
   // sixteen owners' lengths in a thread's registers cost the small calls 2 us

@@ -306,6 +306,28 @@ def test_extend_fills_lists_longer_than_a_block():
         assert got[k] == ref[k], k
 
 
+def test_extend_returns_and_takes_many_pages_without_a_map():
+    """All owners end at once in a large cache: no new rows, 40000 pages; then they grow
+    again past the ring's end, the maps alone too small."""
+    page, MP, N = 16, 900, 41000
+    rng = random.Random(2)
+    have = [16 * 800 - rng.randint(0, 15) for _ in range(50)]
+    deal = rng.sample(range(N), N)
+    table = [deal[800 * r:800 * (r + 1)] + [-5] * 100 for r in range(50)]
+    front = N - 300
+    ring = [-1] * N
+    for i, p in enumerate(deal[40000:]):
+        ring[(front + i) % N] = p
+    for want in ([0] * 50, [rng.choice([0, 5, 16 * 400]) for _ in range(50)]):
+        ref = extend_ref(have, want, front, 1000, table, ring, page, 0)
+        got = run_extend(have, want, front, 1000, table, ring, page, 0)
+        assert ref["result"][0] == 0 and ref["result"][3] > 20000
+        for k in ref:
+            assert got[k] == ref[k], k
+    refused = run_extend([0] * 50, [3] * 50, got["pos"][0], got["pos"][1], got["table"], got["ring"], page, 149)
+    assert refused["result"] == [-7, 0, 0, 0] and refused["ring"] == got["ring"]
+
+
 def test_extend_that_does_not_fit_changes_nothing():
     page, MP = 16, 4
     table = [[0, 1, -5, -5], [2, -5, -5, -5]]
