@@ -455,6 +455,10 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const AppendParams ap) {
 
 constexpr int kSelThreads = 512, kSelWaves = kSelThreads / 64;
 constexpr int kSelRows = 256;            // most rows that several blocks share
+// Pages of a part: below, the exchange costs more than it saves.  64 rows of 2048
+// pages take 19.3, 16.1, 14.8 and 16.0 us in 1, 2, 4 and 8 parts, 66 rows of up to 564
+// pages 8.1 and 8.6 us in 1 and 2.
+constexpr int kSelPart = 512;
 constexpr int kSelBits = 12, kSelBins = 1 << kSelBits;
 
 struct SelectParams {
@@ -509,7 +513,10 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(const SelectPara
     for (int j = split * kSelThreads + tid; j < keep; j += sp.splits * kSelThreads) out[j] = j < np ? j : -1;
     return;
   }
-  const int chunk = ((np + sp.splits - 1) / sp.splits + 1) & ~1;
+  // as many of the row's blocks as its pages are worth
+  const int splits = min(sp.splits, max(1, (np + kSelPart / 2) / kSelPart));
+  if (split >= splits) return;
+  const int chunk = ((np + splits - 1) / splits + 1) & ~1;
   const int j0 = min(np, split * chunk), j1 = min(np, j0 + chunk);
 
   // the first pages' bounds are on their way while the queries are folded:
@@ -591,14 +598,14 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(const SelectPara
   }
   __syncthreads();
 
-  if (sp.splits > 1) {
+  if (splits > 1) {
     uint64_t* shared_key = reinterpret_cast<uint64_t*>(sp.score + size_t(row) * sp.pitch);
     for (int k = j0 / 2 + tid; j0 < j1 && k < (j1 + 1) / 2; k += kSelThreads)
       __hip_atomic_store(shared_key + k, uint64_t(key[2 * k + 1]) << 32 | key[2 * k], __ATOMIC_RELAXED,
                          __HIP_MEMORY_SCOPE_AGENT);
     shared_done();
     __syncthreads();
-    if (tid == 0) pick[0] = count_in(&sp.count[row], uint32_t(sp.splits - 1));
+    if (tid == 0) pick[0] = count_in(&sp.count[row], uint32_t(splits - 1));
     __syncthreads();
     if (!pick[0]) return;
     for (int k = tid; k < (np + 1) / 2; k += kSelThreads) {
@@ -1513,13 +1520,11 @@ hipError_t launch_kv_select(const KvSelectLaunch& L, hipStream_t stream) {
   const KvWorkspace ws(L.workspace, L.s);
   p.count = ws.select_count;
   p.score = ws.score;
-  // Each part with enough pages to be worth the exchange, and about two blocks a CU:
-  // 64 rows of 2048 pages take 19.3, 16.1, 14.8 and 16.0 us in 1, 2, 4 and 8 parts, 66
-  // rows of 564 pages 8.1 and 8.6 us in 1 and 2.
+  // about two blocks a CU
   const int rows = int(L.n) * L.s.kv_heads;
   p.splits = 1;
   if (L.workspace && rows <= select_rows(L.s))
-    while (p.splits < 8 && p.splits * 2 * rows <= 512 && L.s.max_pages / (p.splits * 2) >= 512) p.splits *= 2;
+    while (p.splits < 8 && p.splits * 2 * rows <= 512 && L.s.max_pages / (p.splits * 2) >= kSelPart) p.splits *= 2;
   const dim3 grid(unsigned(rows * p.splits)), block(kSelThreads);
   const size_t lds = size_t(p.pitch) * sizeof(uint32_t);
   auto go = [&](auto kernel) {
