@@ -3,6 +3,7 @@
 // page selection, and one new token's attention.
 
 #include "rwttt_kv_kernels.h"
+#include "rwttt_kv_rules.h"
 
 #include <type_traits>
 
@@ -459,7 +460,6 @@ constexpr int kSelRows = 256;            // most rows that several blocks share
 // pages take 19.3, 16.1, 14.8 and 16.0 us in 1, 2, 4 and 8 parts, 66 rows of up to 564
 // pages 8.1 and 8.6 us in 1 and 2.
 constexpr int kSelPart = 512;
-constexpr int kSelBits = 12, kSelBins = 1 << kSelBits;
 
 struct SelectParams {
   KvSelectLaunch L;
@@ -616,12 +616,12 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(const SelectPara
     __syncthreads();
   }
 
-  // Pages [f0, f1) are ranked, by v = score - least.  To be taken: v > v0, and of
-  // those equal to v0 the first `want`.
+  // Pages [f0, f1) are ranked, by v = score - least (rwttt_kv_rules.h).  None is to be
+  // taken: no v reaches above ~0.
   const int f0 = int(p.first), f1 = np - int(p.last);
-  int want = keep - (np - (f1 - f0));
-  uint32_t least = ~0u, v0 = ~0u;
-  if (want > 0) {
+  Rank rank{~0u, 0, 0};
+  uint32_t least = ~0u;
+  if (const int want = keep - (np - (f1 - f0)); want > 0) {
     uint32_t most = 0;
     for (int j = f0 + tid; j < f1; j += kSelThreads) {
       least = min(least, key[j]);
@@ -639,9 +639,8 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(const SelectPara
       least = min(least, wave_range[w].x);
       most = max(most, wave_range[w].y);
     }
-    v0 = 0;
-    for (int top = most == least ? 0 : 32 - __clz(int(most - least)); top > 0;) {
-      const int bit = max(0, top - kSelBits);
+    rank = rank_begin(most - least, want);
+    while (rank.top > 0) {
       constexpr int PER = kSelBins / kSelThreads;
       for (int k = tid; k < kSelBins / 4; k += kSelThreads)
         *reinterpret_cast<u32x4_t*>(hist + 4 * k) = (u32x4_t){0, 0, 0, 0};
@@ -649,7 +648,7 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(const SelectPara
       __syncthreads();
       for (int j = f0 + tid; j < f1; j += kSelThreads) {
         const uint32_t v = key[j] - least;
-        if (top == 32 || v >> top == v0 >> top) atomicAdd(&hist[(v >> bit) & (kSelBins - 1)], 1u);
+        if (rank_in(rank, v)) atomicAdd(&hist[rank_bin(rank, v)], 1u);
       }
       __syncthreads();
       uint32_t c[PER], sum = 0;          // the thread's bins, from the top
@@ -658,27 +657,20 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(const SelectPara
       uint32_t above = block_scan(sum, wave_sum[0]);
 #pragma unroll
       for (int k = 0; k < PER; ++k) {
-        if (above < uint32_t(want) && above + c[k] >= uint32_t(want)) {
+        if (above < uint32_t(rank.want) && above + c[k] >= uint32_t(rank.want)) {
           pick[0] = uint32_t(kSelBins - 1 - (tid * PER + k));
-          pick[1] = uint32_t(want) - above;
+          pick[1] = above;
           pick[2] = c[k];
         }
         above += c[k];
       }
       __syncthreads();
-      v0 |= pick[0] << bit;
-      want = int(pick[1]);
       const uint32_t in_bin = pick[2];
-      top = bit;
-      if (in_bin == uint32_t(want)) {    // the whole bin
-        v0 = v0 ? v0 - 1 : 0;
-        want = v0 ? 0 : want;
-        break;
-      }
-      if (top > 0 && in_bin <= uint32_t(kSelThreads)) {
+      rank = rank_narrow(rank, pick[0], int(pick[1]), int(in_bin));
+      if (rank.top > 0 && in_bin <= uint32_t(kSelThreads)) {
         for (int j = f0 + tid; j < f1; j += kSelThreads) {
           const uint32_t v = key[j] - least;
-          if (v >> top == v0 >> top) close[atomicAdd(&pick[3], 1u)] = make_uint2(v, uint32_t(j));
+          if (rank_in(rank, v)) close[atomicAdd(&pick[3], 1u)] = make_uint2(v, uint32_t(j));
         }
         __syncthreads();
         if (uint32_t(tid) < in_bin) {
@@ -689,19 +681,19 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(const SelectPara
             larger += x.x > mine.x;
             before += x.x == mine.x && x.y < mine.y;
           }
-          if (larger + before == uint32_t(want) - 1) {   // the last page kept
+          if (larger + before == uint32_t(rank.want) - 1) {   // the last page kept
             pick[0] = mine.x;
             pick[1] = before + 1;
           }
         }
         __syncthreads();
-        v0 = pick[0];
-        want = int(pick[1]);
-        break;
+        rank = Rank{pick[0], int(pick[1]), 0};
       }
       __syncthreads();
     }
   }
+  const uint32_t v0 = rank.v0;
+  const int want = rank.want;
 
   // in order
   const int per = (np + kSelThreads - 1) / kSelThreads, p0 = min(np, tid * per), p1 = min(np, p0 + per);

@@ -1,0 +1,40 @@
+"""The paged cache's device rules on the CPU: a small program over the library's own header
+answers one query per line."""
+
+import os
+import random
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def ask(tmp_path_factory):
+    exe = str(tmp_path_factory.mktemp("kv_rules") / "kv_rules_check")
+    subprocess.run(["g++", "-std=c++17", "-Wall", "-Werror", "-I", os.path.join(ROOT, "paper_2605_28053_amd", "csrc"),
+                    os.path.join(ROOT, "tests", "c", "kv_rules_check.cpp"), "-o", exe], check=True)
+
+    def query(lines):
+        out = subprocess.run([exe], input="\n".join(lines) + "\n", capture_output=True, text=True, check=True)
+        answers = out.stdout.splitlines()
+        assert len(answers) == len(lines)
+        return [[int(x) for x in a.split()] for a in answers]
+    return query
+
+
+@pytest.mark.parametrize("spread", [1, 2, 3, 5, 40, 4095, 4096, 4097, 10 ** 6, 2 ** 31, 2 ** 32 - 1])
+@pytest.mark.parametrize("close", [0, 6, 512])
+def test_the_ranking_keeps_the_largest_scores(ask, spread, close):
+    """Every number kept, of scores that tie, are neighbours, or span all 32 bits."""
+    rng = random.Random(spread + close)
+    cases = []
+    for n in (2, 3, 17, 65, 200):
+        for _ in range(6):
+            base = -(spread // 2)
+            score = [base + rng.choice([0, 1, 2, rng.randint(0, spread), spread]) % (spread + 1) for _ in range(n)]
+            cases += [(want, score) for want in sorted({1, 2, n // 2, n - 2, n - 1} & set(range(1, n)))]
+    got = ask([f"rank {want} {close} {len(s)} {' '.join(map(str, s))}" for want, s in cases])
+    for (want, s), kept in zip(cases, got):
+        assert kept == sorted(sorted(range(len(s)), key=lambda j: (-s[j], j))[:want]), (want, s)
