@@ -771,13 +771,6 @@ constexpr int kAttPad = 4;               // floats behind a query's sums in LDS:
 // Rows of keys a wave takes at a time.
 constexpr int tile_rows(int ct) { return ct == RWTTT_F32 ? 16 : 32; }
 
-// A row's fixed cost in tiles: finding its pages, starting its loads and adding
-// the waves' sums.  Counted in the line that is cut, it keeps a block from being
-// dealt dozens of short rows against another's one long one: 32 owners of 1 to
-// 40000 rows in e4m3 take 150 us without it, 115, 101, 88, 90 and 91 us with 2,
-// 4, 8, 16 and 24 tiles.
-constexpr int kRowCost = 8;
-
 struct RowRange {
   int base, tiles, held;                 // base: first tile's first row; held: listed pages
 };
@@ -813,7 +806,7 @@ __device__ __forceinline__ void fill_rows(const KvAttendLaunch& p, const RowTabl
   const int per = (n + kAttThreads - 1) / kAttThreads, i0 = min(n, tid * per), i1 = min(n, i0 + per);
   auto cost = [&](int len) {
     const int tiles = row_range<KT>(p, len).tiles;
-    return uint32_t(tiles ? tiles + kRowCost : 0);
+    return row_cost(tiles);
   };
   uint32_t sum = 0;
   for (int i = i0; i < i1; ++i) {
@@ -835,45 +828,6 @@ __device__ __forceinline__ void fill_rows(const KvAttendLaunch& p, const RowTabl
   }
   if (i1 == n && i0 < n) rt.pre[n] = at;
   __syncthreads();
-}
-
-// Part w of [0, total) cut into `parts` parts, the first ones one longer.
-struct Cut {
-  uint64_t per, rem;
-  __device__ Cut(uint64_t total, int parts) {
-    if (total >> 32) {                   // 64-bit division is a long routine
-      per = total / parts;
-      rem = total % parts;
-    } else {
-      per = uint32_t(total) / uint32_t(parts);
-      rem = uint32_t(total) % uint32_t(parts);
-    }
-  }
-  __device__ uint64_t begin(uint64_t w) const { return w * per + min(w, rem); }
-  __device__ int part_of(uint64_t u) const {
-    const uint64_t head = rem * (per + 1);
-    const uint64_t x = u < head ? u : u - head, by = u < head ? per + 1 : per;
-    const uint64_t at = x >> 32 || by >> 32 ? x / by : uint32_t(x) / uint32_t(by);
-    return int(u < head ? at : rem + at);
-  }
-};
-
-// Smallest part of the line: a short row, or a few tiles of a long one.  One owner
-// of 4224 rows takes 15.0, 13.5, 13.1 and 13.3 us with 4, 6, 8 and 12: smaller parts
-// have more results to join.
-constexpr int kPartCost = 8;
-__device__ __forceinline__ int parts_of(uint64_t total, int blocks) {
-  return total >= uint64_t(blocks) * kPartCost ? blocks : int(uint32_t(total + kPartCost - 1) / kPartCost);
-}
-
-// A cut that falls in a short row, or near an end of a long one, moves to the
-// row's end: joining costs more than the imbalance (64 owners of up to 300 rows 17.2
-// -> 13.4 us; 24 tiles as the bound of a short row measure the same).
-constexpr uint32_t kShortRow = kRowCost + 12, kRowHead = kRowCost + 3, kRowTail = 3;
-static_assert(kShortRow > kRowHead + kRowTail, "a row that is split keeps a middle");
-__device__ __forceinline__ uint32_t snapped(uint32_t x, uint32_t cost) {
-  if (cost <= kShortRow || x <= kRowHead) return 0;
-  return x >= cost - kRowTail ? cost : x;
 }
 
 template <int W, bool HINT = false> __device__ __forceinline__ void load_words(const char* p, uint32_t* w) {
@@ -1308,7 +1262,7 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
       // its first block, since only the last row of a block's part can go on behind
       // it; of a window, one for the row that began before it and one for the row
       // that begins in it and goes on.
-      const int b0 = cut.part_of(u0 + kRowHead), b1 = cut.part_of(u0 + cost - kRowTail - 1);
+      const int b0 = first_part(cut, u0), b1 = last_part(cut, u0, cost);
       const int w = b / kJoinWindow, w0 = b0 / kJoinWindow, w1 = b1 / kJoinWindow;
       bool final = b1 - b0 < kJoinDirect;
       int k0 = final ? b0 : max(b0, w * kJoinWindow), k1 = final ? b1 : min(b1, (w + 1) * kJoinWindow - 1);
@@ -1471,11 +1425,8 @@ template <int IO, int CT> hipError_t append_dims(const AppendParams& p, hipStrea
 }
 
 template <int IO, int CT, int D> hipError_t attend_go(AttendParams p, hipStream_t stream) {
-  // no more blocks than the longest owners could give tiles to, and one for each
-  // owner without rows
-  const uint64_t rows = uint64_t(p.L.s.max_pages) << p.L.s.page_shift;
-  const uint64_t tiles = uint64_t(p.L.n) * p.L.s.kv_heads * p.head_tiles * ((rows + 15) / 16);
-  const dim3 grid(unsigned(tiles < uint64_t(p.blocks) ? tiles : p.blocks));
+  const uint64_t rows = uint64_t(p.L.n) * p.L.s.kv_heads * p.head_tiles;
+  const dim3 grid(unsigned(attend_grid(rows, p.L.s.max_pages << p.L.s.page_shift, tile_rows(CT), p.blocks)));
   const int acc = kAttWaves * p.part_heads * (D + kAttPad), join = kAttThreads * 6;
   p.acc_words = acc < join ? join : acc;
   const size_t lds = (p.acc_words + row_table_words(int(p.L.n))) * sizeof(float);

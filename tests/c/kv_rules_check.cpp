@@ -1,6 +1,9 @@
 // Prints the answers of the paged cache's rules, one line for each query line of stdin:
 //   rank want close n s0 .. s(n-1)   -> the kept indices; bins of at most `close` scores are
 //                                       ranked one by one
+//   cut blocks vh tile longest n l0 .. l(n-1) -> blocks launched, parts, parts of no block, tiles
+//                                       that are not held by one launched part alone, rows whose
+//                                       first and last part are not those that hold them
 #include <algorithm>
 #include <cstdio>
 #include <iostream>
@@ -40,6 +43,47 @@ static void rank(int want, int close, const std::vector<long long>& score) {
   std::printf("\n");
 }
 
+// attend's walk of the line of n owners' rows (vh each), the parts one after another.
+static void cut_line(int blocks, int vh, int tile, int longest, const std::vector<int>& len) {
+  const int n = int(len.size());
+  std::vector<uint64_t> pre(n + 1);
+  for (int i = 0; i < n; ++i) pre[i + 1] = pre[i] + row_cost((len[i] + tile - 1) / tile);
+  const uint64_t total = pre[n] * vh;
+  const int grid = attend_grid(uint64_t(n) * vh, longest, tile, blocks), parts = parts_of(total, blocks);
+  std::vector<std::vector<int>> held(size_t(n) * vh);       // launched parts that hold each tile
+  std::vector<std::vector<int>> by(size_t(n) * vh);         // parts that hold some of the row
+  for (int r = 0; r < n * vh; ++r) held[r].resize((len[r / vh] + tile - 1) / tile);
+  const Cut cut(total ? total : 1, parts ? parts : 1);
+  auto begin = [&](int b) {
+    const uint64_t u = cut.begin(b);
+    if (u >= total) return total;
+    int i = 0;
+    while (pre[i + 1] * vh <= u) ++i;
+    const uint32_t cost = uint32_t(pre[i + 1] - pre[i]), x = uint32_t(u - pre[i] * vh) % cost;
+    return u + snapped(x, cost) - x;
+  };
+  for (int b = 0; b < std::min(grid, parts); ++b) {
+    const uint64_t u = begin(b), end = begin(b + 1);
+    for (int r = 0; r < n * vh; ++r) {
+      const uint64_t u0 = pre[r / vh] * vh + (r % vh) * (pre[r / vh + 1] - pre[r / vh]);
+      const uint64_t cost = pre[r / vh + 1] - pre[r / vh], x0 = std::max(u, u0), x1 = std::min(end, u0 + cost);
+      if (x0 >= x1) continue;
+      by[r].push_back(b);
+      for (uint64_t t = std::max<int64_t>(0, int64_t(x0 - u0) - kRowCost); int64_t(t) < int64_t(x1 - u0) - kRowCost; ++t)
+        ++held[r][t];
+    }
+  }
+  int wrong = 0, joins = 0;
+  for (int r = 0; r < n * vh; ++r) {
+    for (int x : held[r]) wrong += x != 1;
+    if (held[r].empty() || by[r].size() == 1) continue;
+    const uint64_t u0 = pre[r / vh] * vh + (r % vh) * (pre[r / vh + 1] - pre[r / vh]);
+    const int b0 = first_part(cut, u0), b1 = last_part(cut, u0, uint32_t(pre[r / vh + 1] - pre[r / vh]));
+    joins += by[r].empty() || by[r].front() != b0 || by[r].back() != b1 || int(by[r].size()) != b1 - b0 + 1;
+  }
+  std::printf("%d %d %d %d %d\n", grid, parts, std::max(0, parts - grid), wrong, joins);
+}
+
 int main() {
   std::string what;
   while (std::cin >> what) {
@@ -49,6 +93,12 @@ int main() {
       std::vector<long long> score(n);
       for (long long& s : score) std::cin >> s;
       rank(want, close, score);
+    } else if (what == "cut") {
+      int blocks, vh, tile, longest, n;
+      std::cin >> blocks >> vh >> tile >> longest >> n;
+      std::vector<int> len(n);
+      for (int& l : len) std::cin >> l;
+      cut_line(blocks, vh, tile, longest, len);
     }
   }
 }

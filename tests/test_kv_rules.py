@@ -38,3 +38,22 @@ def test_the_ranking_keeps_the_largest_scores(ask, spread, close):
     got = ask([f"rank {want} {close} {len(s)} {' '.join(map(str, s))}" for want, s in cases])
     for (want, s), kept in zip(cases, got):
         assert kept == sorted(sorted(range(len(s)), key=lambda j: (-s[j], j))[:want]), (want, s)
+
+
+@pytest.mark.parametrize("tile", [16, 32])
+@pytest.mark.parametrize("longest", [16, 32, 48, 64, 256, 4096])
+def test_every_tile_is_held_by_one_block_that_is_launched(ask, tile, longest):
+    """The smallest caches, one 16-row page an owner, to those whose rows are split: all
+    owners as long as they may be, of one row, and ragged with empty ones."""
+    rng = random.Random(tile + longest)
+    lines = []
+    for n in (1, 2, 3, 7, 8, 64, 65, 480, 700):
+        for vh in (1, 2, 8, 24):
+            if n * vh > 2000:
+                continue
+            for lens in ([longest] * n, [1] * n, [rng.choice([0, 1, 15, 16, 17, rng.randint(0, longest)]) % (longest + 1)
+                                                  for _ in range(n)]):
+                for blocks in (256, 512):
+                    lines.append(f"cut {blocks} {vh} {tile} {longest} {n} {' '.join(map(str, lens))}")
+    for line, (grid, parts, lost, wrong, joins) in zip(lines, ask(lines)):
+        assert (lost, wrong, joins) == (0, 0, 0) and 1 <= grid <= 512, line[:80]
