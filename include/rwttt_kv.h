@@ -152,7 +152,7 @@ rwttt_status rwttt_kv_append(rwttt_kv* kv, uint32_t layer, const void* k, uint64
  * The score bounds what the page's keys can add to the logits of the head's
  * (rounded) queries together.  With a the largest magnitude in the group's queries and
  * q8 = rint(q * ((1 / a) * 127)), each step rounded to fp32 (0 for a = 0, or so
- * small that 1 / a overflows),
+ * small, below 3.8e-37, that (1 / a) * 127 overflows),
  *     score = sum over the group's queries and channels of max(q8 lo, q8 hi):
  * whole numbers, so that the choice is exact; ties go to the lowest page.
  * Queries that are not finite select some pages, not specified which.

@@ -550,7 +550,7 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(const SelectPara
   __syncthreads();
   a = 0.f;
   for (int w = 0; w < kSelWaves; ++w) a = fmaxf(a, wave_max[w]);
-  const float inv = 1.f / a, to = a > 0.f && inv < INFINITY ? inv * 127.f : 0.f;
+  const float to = query_unit(a);
   if (tid < D) {
     int up = 0, down = 0;
     for (int g = 0; g < G; ++g) {

@@ -11,6 +11,13 @@ namespace rwttt {
 // select: which scores are kept
 // ---------------------------------------------------------------------------
 
+// What the queries of a group, with a the largest magnitude, are multiplied by before
+// they are rounded to 8 bits.  Queries so small that it is no fp32 number count as 0.
+constexpr float query_unit(float a) {
+  const float to = a > 0.f ? 1.f / a * 127.f : 0.f;
+  return to < __builtin_inff() ? to : 0.f;
+}
+
 constexpr int kSelBits = 12, kSelBins = 1 << kSelBits;
 
 // The state of a ranking of v = score - least, narrowed by the bin that the last

@@ -1,11 +1,14 @@
 // Prints the answers of the paged cache's rules, one line for each query line of stdin:
 //   rank want close n s0 .. s(n-1)   -> the kept indices; bins of at most `close` scores are
 //                                       ranked one by one
+//   unit a                           -> query_unit's bits
 //   cut blocks vh tile longest n l0 .. l(n-1) -> blocks launched, parts, parts of no block, tiles
 //                                       that are not held by one launched part alone, rows whose
 //                                       first and last part are not those that hold them
 #include <algorithm>
 #include <cstdio>
+#include <cstdlib>
+#include <cstring>
 #include <iostream>
 #include <string>
 #include <vector>
@@ -93,6 +96,13 @@ int main() {
       std::vector<long long> score(n);
       for (long long& s : score) std::cin >> s;
       rank(want, close, score);
+    } else if (what == "unit") {
+      std::string text;
+      std::cin >> text;
+      const float unit = query_unit(std::strtof(text.c_str(), nullptr));
+      uint32_t bits;
+      std::memcpy(&bits, &unit, 4);
+      std::printf("%u\n", bits);
     } else if (what == "cut") {
       int blocks, vh, tile, longest, n;
       std::cin >> blocks >> vh >> tile >> longest >> n;

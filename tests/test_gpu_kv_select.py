@@ -88,3 +88,19 @@ def test_coarse_bounds(io, cache, n, keep):
         check(c, one, b, keep, 1, 2)
     assert np.unique(b.numpy()).size < 12
     c.close()
+
+
+@pytest.mark.parametrize("io,cache", [("bf16", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("size", [0.0, 1e-39, 3e-39, 1e-37, 3.5e-37])
+def test_queries_too_small_for_a_unit_tie(io, cache, size):
+    """All scores are 0 then, whatever the channels hold: the lowest pages, and the forced ones."""
+    n, keep = 40, 9
+    c = Cache([16 * n - 3] * 3, H=2, G=2, D=64, page=16, io=io, cache=cache, seed=3, poison=False)
+    b = torch.randint(-90, 91, c.bounds_h.shape, dtype=torch.int8, generator=torch.Generator().manual_seed(1))
+    c.bounds.copy_(b.sort(dim=2).values)
+    q = torch.zeros_like(c.q_h)
+    q[:, :, ::3] = size
+    q[:, :, 1::3] = -size / 2
+    got = select(c, q, keep, 1, 2)
+    assert (got == torch.tensor(list(range(keep - 2)) + [n - 2, n - 1], dtype=torch.int32)).all()
+    c.close()

@@ -5,6 +5,7 @@ import os
 import random
 import subprocess
 
+import numpy as np
 import pytest
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -57,3 +58,18 @@ def test_every_tile_is_held_by_one_block_that_is_launched(ask, tile, longest):
                     lines.append(f"cut {blocks} {vh} {tile} {longest} {n} {' '.join(map(str, lens))}")
     for line, (grid, parts, lost, wrong, joins) in zip(lines, ask(lines)):
         assert (lost, wrong, joins) == (0, 0, 0) and 1 <= grid <= 512, line[:80]
+
+
+def test_the_queries_unit_is_a_number(ask):
+    """(1 / a) 127, or 0 where that overflows: the smallest magnitudes."""
+    with np.errstate(over="ignore", divide="ignore"):
+        values = [np.float32(x) for x in (0, 1e-45, 2.8e-39, 3e-39, 1e-38, 1e-37, 3.7e-37, 3.74e-37, 4e-37, 1e-30, 1, 127, 3e38)]
+        for a, (bits,) in zip(values, ask([f"unit {float(a)!r}" for a in values])):
+            to = np.float32(1) / a * np.float32(127) if a > 0 else np.float32(0)
+            want = to if np.isfinite(to) else np.float32(0)
+            assert np.uint32(bits).view(np.float32) == want, a
+
+
+def test_queries_whose_unit_overflows_count_as_zero(ask):
+    (bits,), (some,) = ask(["unit 1e-37", "unit 4e-37"])
+    assert bits == 0 and some != 0
