@@ -454,7 +454,6 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const AppendParams ap) {
 // 14.8 us, of which the bounds' loads 9.7 (a plain read of as much: 4.6), the
 // exchange between the blocks 2, the ranking 2.5; one block a row takes 19.3 us.
 
-constexpr int kSelThreads = 512, kSelWaves = kSelThreads / 64;
 constexpr int kSelRows = 256;            // most rows that several blocks share
 // Pages of a part: below, the exchange costs more than it saves.  64 rows of 2048
 // pages take 19.3, 16.1, 14.8 and 16.0 us in 1, 2, 4 and 8 parts, 66 rows of up to 564
@@ -494,13 +493,7 @@ template <int IO, int D>
 __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(const SelectParams sp) {
   const KvSelectLaunch& p = sp.L;
   extern __shared__ uint32_t key[];      // [pitch] scores, ordered as unsigned numbers
-  __shared__ uint32_t digits[4][D / 4];  // U's low and high digit, V's low and high digit
-  __shared__ uint32_t hist[kSelBins];
-  __shared__ uint2 close[kSelThreads];   // score and page
-  __shared__ float wave_max[kSelWaves];
-  __shared__ uint2 wave_range[kSelWaves];
-  __shared__ uint32_t wave_sum[2][kSelWaves];
-  __shared__ uint32_t pick[4];
+  __shared__ SelectLds<D> lds;
   const int H = p.s.kv_heads, G = p.s.group, shift = p.s.page_shift, P = 1 << shift;
   const int row = blockIdx.x / sp.splits, split = blockIdx.x % sp.splits, i = row / H, h = row % H;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -546,10 +539,10 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(const SelectPara
   }
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) a = fmaxf(a, __shfl_xor(a, d));
-  if (lane == 0) wave_max[wave] = a;
+  if (lane == 0) lds.wave_max[wave] = a;
   __syncthreads();
   a = 0.f;
-  for (int w = 0; w < kSelWaves; ++w) a = fmaxf(a, wave_max[w]);
+  for (int w = 0; w < kSelWaves; ++w) a = fmaxf(a, lds.wave_max[w]);
   const float to = query_unit(a);
   if (tid < D) {
     int up = 0, down = 0;
@@ -559,7 +552,7 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(const SelectPara
       up += max(q8, 0);
       down += max(-q8, 0);
     }
-    uint8_t* dg = reinterpret_cast<uint8_t*>(digits);
+    uint8_t* dg = reinterpret_cast<uint8_t*>(lds.digits);
     dg[tid] = uint8_t(up & 127);
     dg[D + tid] = uint8_t(up >> 7);
     dg[2 * D + tid] = uint8_t(down & 127);
@@ -572,8 +565,8 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(const SelectPara
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
     const int at = (piece % (LPP / 2)) * 4 + w;
-    d0[w] = int(digits[low ? 2 : 0][at]);
-    d1[w] = int(digits[low ? 3 : 1][at]);
+    d0[w] = int(lds.digits[low ? 2 : 0][at]);
+    d1[w] = int(lds.digits[low ? 3 : 1][at]);
   }
   for (; base < j1; base += kSelWaves * PPI * U) {
     int s[U];
@@ -605,9 +598,9 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(const SelectPara
                          __HIP_MEMORY_SCOPE_AGENT);
     shared_done();
     __syncthreads();
-    if (tid == 0) pick[0] = count_in(&sp.count[row], uint32_t(splits - 1));
+    if (tid == 0) lds.pick[0] = count_in(&sp.count[row], uint32_t(splits - 1));
     __syncthreads();
-    if (!pick[0]) return;
+    if (!lds.pick[0]) return;
     for (int k = tid; k < (np + 1) / 2; k += kSelThreads) {
       const uint64_t w = __hip_atomic_load(shared_key + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       key[2 * k] = uint32_t(w);
@@ -632,62 +625,65 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(const SelectPara
       least = min(least, uint32_t(__shfl_xor(int(least), d)));
       most = max(most, uint32_t(__shfl_xor(int(most), d)));
     }
-    if (lane == 0) wave_range[wave] = make_uint2(least, most);
+    if (lane == 0) {
+      lds.wave_least[wave] = least;
+      lds.wave_most[wave] = most;
+    }
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kSelWaves; ++w) {
-      least = min(least, wave_range[w].x);
-      most = max(most, wave_range[w].y);
+      least = min(least, lds.wave_least[w]);
+      most = max(most, lds.wave_most[w]);
     }
     rank = rank_begin(most - least, want);
     while (rank.top > 0) {
       constexpr int PER = kSelBins / kSelThreads;
       for (int k = tid; k < kSelBins / 4; k += kSelThreads)
-        *reinterpret_cast<u32x4_t*>(hist + 4 * k) = (u32x4_t){0, 0, 0, 0};
-      if (tid == 0) pick[3] = 0;
+        *reinterpret_cast<u32x4_t*>(lds.hist + 4 * k) = (u32x4_t){0, 0, 0, 0};
+      if (tid == 0) lds.pick[3] = 0;
       __syncthreads();
       for (int j = f0 + tid; j < f1; j += kSelThreads) {
         const uint32_t v = key[j] - least;
-        if (rank_in(rank, v)) atomicAdd(&hist[rank_bin(rank, v)], 1u);
+        if (rank_in(rank, v)) atomicAdd(&lds.hist[rank_bin(rank, v)], 1u);
       }
       __syncthreads();
       uint32_t c[PER], sum = 0;          // the thread's bins, from the top
 #pragma unroll
-      for (int k = 0; k < PER; ++k) sum += c[k] = hist[kSelBins - 1 - (tid * PER + k)];
-      uint32_t above = block_scan(sum, wave_sum[0]);
+      for (int k = 0; k < PER; ++k) sum += c[k] = lds.hist[kSelBins - 1 - (tid * PER + k)];
+      uint32_t above = block_scan(sum, lds.wave_sum[0]);
 #pragma unroll
       for (int k = 0; k < PER; ++k) {
         if (above < uint32_t(rank.want) && above + c[k] >= uint32_t(rank.want)) {
-          pick[0] = uint32_t(kSelBins - 1 - (tid * PER + k));
-          pick[1] = above;
-          pick[2] = c[k];
+          lds.pick[0] = uint32_t(kSelBins - 1 - (tid * PER + k));
+          lds.pick[1] = above;
+          lds.pick[2] = c[k];
         }
         above += c[k];
       }
       __syncthreads();
-      const uint32_t in_bin = pick[2];
-      rank = rank_narrow(rank, pick[0], int(pick[1]), int(in_bin));
+      const uint32_t in_bin = lds.pick[2];
+      rank = rank_narrow(rank, lds.pick[0], int(lds.pick[1]), int(in_bin));
       if (rank.top > 0 && in_bin <= uint32_t(kSelThreads)) {
         for (int j = f0 + tid; j < f1; j += kSelThreads) {
           const uint32_t v = key[j] - least;
-          if (rank_in(rank, v)) close[atomicAdd(&pick[3], 1u)] = make_uint2(v, uint32_t(j));
+          if (rank_in(rank, v)) lds.close[atomicAdd(&lds.pick[3], 1u)] = ScoredPage{v, uint32_t(j)};
         }
         __syncthreads();
         if (uint32_t(tid) < in_bin) {
-          const uint2 mine = close[tid];
+          const ScoredPage mine = lds.close[tid];
           uint32_t larger = 0, before = 0;
           for (uint32_t k = 0; k < in_bin; ++k) {
-            const uint2 x = close[k];
-            larger += x.x > mine.x;
-            before += x.x == mine.x && x.y < mine.y;
+            const ScoredPage x = lds.close[k];
+            larger += x.score > mine.score;
+            before += x.score == mine.score && x.page < mine.page;
           }
           if (larger + before == uint32_t(rank.want) - 1) {   // the last page kept
-            pick[0] = mine.x;
-            pick[1] = before + 1;
+            lds.pick[0] = mine.score;
+            lds.pick[1] = before + 1;
           }
         }
         __syncthreads();
-        rank = Rank{pick[0], int(pick[1]), 0};
+        rank = Rank{lds.pick[0], int(lds.pick[1]), 0};
       }
       __syncthreads();
     }
@@ -703,7 +699,7 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(const SelectPara
     const uint32_t v = key[j] - least;
     count += forced || v > v0 ? 1u : v == v0 ? 0x10000u : 0u;
   }
-  const uint32_t at = block_scan(count, wave_sum[1]);
+  const uint32_t at = block_scan(count, lds.wave_sum[1]);
   int so = int(at & 0xffffu), se = int(at >> 16);
   for (int j = p0; j < p1; ++j) {
     const bool forced = j < f0 || j >= f1;
@@ -1348,8 +1344,6 @@ constexpr int kAttBlocks = 512;          // two a CU
 
 int part_heads_of(int group) { return group < 16 ? group : 16; }
 
-int select_pitch(int max_pages) { return (max_pages + 1) & ~1; }
-
 // Rows (an owner and kv head) that several blocks may share in a select.
 int select_rows(const KvShape& s) {
   if (s.max_pages > RWTTT_KV_MAX_SELECT) return 0;
@@ -1470,9 +1464,9 @@ hipError_t launch_kv_select(const KvSelectLaunch& L, hipStream_t stream) {
   if (L.workspace && rows <= select_rows(L.s))
     while (p.splits < 8 && p.splits * 2 * rows <= 512 && L.s.max_pages / (p.splits * 2) >= kSelPart) p.splits *= 2;
   const dim3 grid(unsigned(rows * p.splits)), block(kSelThreads);
-  const size_t lds = size_t(p.pitch) * sizeof(uint32_t);
-  auto go = [&](auto kernel) {
-    if (lds > 48 * 1024) {               // more than 64 KB of the CU's 160 KB has to be asked for
+  const size_t lds = select_lds(L.s.max_pages);
+  auto go = [&](auto kernel, bool asks) {
+    if (asks) {
       const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                                hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
       if (e != hipSuccess) return e;
@@ -1480,13 +1474,14 @@ hipError_t launch_kv_select(const KvSelectLaunch& L, hipStream_t stream) {
     hipLaunchKernelGGL(kernel, grid, block, lds, stream, p);
     return hipGetLastError();
   };
+  const int pages = L.s.max_pages;
   if (L.s.io_bf16)
-    return L.s.head_dim == 64    ? go(kv_select_kernel<1, 64>)
-           : L.s.head_dim == 128 ? go(kv_select_kernel<1, 128>)
-                                 : go(kv_select_kernel<1, 256>);
-  return L.s.head_dim == 64    ? go(kv_select_kernel<0, 64>)
-         : L.s.head_dim == 128 ? go(kv_select_kernel<0, 128>)
-                               : go(kv_select_kernel<0, 256>);
+    return L.s.head_dim == 64    ? go(kv_select_kernel<1, 64>, select_asks_for_lds<64>(pages))
+           : L.s.head_dim == 128 ? go(kv_select_kernel<1, 128>, select_asks_for_lds<128>(pages))
+                                 : go(kv_select_kernel<1, 256>, select_asks_for_lds<256>(pages));
+  return L.s.head_dim == 64    ? go(kv_select_kernel<0, 64>, select_asks_for_lds<64>(pages))
+         : L.s.head_dim == 128 ? go(kv_select_kernel<0, 128>, select_asks_for_lds<128>(pages))
+                               : go(kv_select_kernel<0, 256>, select_asks_for_lds<256>(pages));
 }
 
 hipError_t launch_kv_attend(const KvAttendLaunch& L, hipStream_t stream) {

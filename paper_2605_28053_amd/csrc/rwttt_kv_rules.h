@@ -3,9 +3,13 @@
 // machine.
 #pragma once
 
+#include <stddef.h>
 #include <stdint.h>
 
 namespace rwttt {
+
+// More LDS than this in a launch has to be asked for; a CU has 160 KB.
+constexpr size_t kPlainLds = 64 * 1024;
 
 // ---------------------------------------------------------------------------
 // select: which scores are kept
@@ -19,6 +23,29 @@ constexpr float query_unit(float a) {
 }
 
 constexpr int kSelBits = 12, kSelBins = 1 << kSelBits;
+
+constexpr int kSelThreads = 512, kSelWaves = kSelThreads / 64;
+
+struct alignas(8) ScoredPage {
+  uint32_t score, page;
+};
+
+// A block's LDS beside its scores (4 bytes a page, the launch's dynamic part).
+template <int D> struct SelectLds {
+  alignas(16) uint32_t hist[kSelBins];
+  alignas(16) uint32_t digits[4][D / 4];   // U's low and high digit, V's low and high digit
+  ScoredPage close[kSelThreads];
+  uint32_t wave_least[kSelWaves], wave_most[kSelWaves], wave_sum[2][kSelWaves];
+  float wave_max[kSelWaves];
+  uint32_t pick[4];
+};
+
+// Scores of a table of max_pages pages, an even number of them.
+constexpr int select_pitch(int max_pages) { return (max_pages + 1) & ~1; }
+constexpr size_t select_lds(int max_pages) { return size_t(select_pitch(max_pages)) * sizeof(uint32_t); }
+template <int D> constexpr bool select_asks_for_lds(int max_pages) {
+  return select_lds(max_pages) + sizeof(SelectLds<D>) > kPlainLds;
+}
 
 // The state of a ranking of v = score - least, narrowed by the bin that the last
 // kept one lies in.  Kept are all v > v0, and of those equal to v0 the first `want`.

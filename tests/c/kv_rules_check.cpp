@@ -1,6 +1,7 @@
 // Prints the answers of the paged cache's rules, one line for each query line of stdin:
 //   rank want close n s0 .. s(n-1)   -> the kept indices; bins of at most `close` scores are
 //                                       ranked one by one
+//   lds dim max_pages                -> bytes of LDS of a select's block, 1 if they are asked for
 //   unit a                           -> query_unit's bits
 //   cut blocks vh tile longest n l0 .. l(n-1) -> blocks launched, parts, parts of no block, tiles
 //                                       that are not held by one launched part alone, rows whose
@@ -96,6 +97,14 @@ int main() {
       std::vector<long long> score(n);
       for (long long& s : score) std::cin >> s;
       rank(want, close, score);
+    } else if (what == "lds") {
+      int dim, pages;
+      std::cin >> dim >> pages;
+      const size_t fixed = dim == 64 ? sizeof(SelectLds<64>) : dim == 128 ? sizeof(SelectLds<128>) : sizeof(SelectLds<256>);
+      const bool asks = dim == 64    ? select_asks_for_lds<64>(pages)
+                        : dim == 128 ? select_asks_for_lds<128>(pages)
+                                     : select_asks_for_lds<256>(pages);
+      std::printf("%zu %d\n", fixed + select_lds(pages), asks);
     } else if (what == "unit") {
       std::string text;
       std::cin >> text;

@@ -104,3 +104,16 @@ def test_queries_too_small_for_a_unit_tie(io, cache, size):
     got = select(c, q, keep, 1, 2)
     assert (got == torch.tensor(list(range(keep - 2)) + [n - 2, n - 1], dtype=torch.int32)).all()
     c.close()
+
+
+@pytest.mark.parametrize("max_pages", [10960, 11500, 12288, 12289])
+@pytest.mark.parametrize("D", [64, 256])
+def test_tables_around_64_kb_of_lds(max_pages, D):
+    """Where a block's scores and its other LDS pass what a launch has without asking."""
+    c = Cache([16 * 1300, 16 * 40 - 3], H=1, G=2, D=D, page=16, io="bf16", cache="fp8", seed=D, poison=False,
+              max_pages=max_pages)
+    g = torch.Generator().manual_seed(1)
+    b = torch.randint(-90, 91, c.bounds_h.shape, dtype=torch.int8, generator=g).sort(dim=2).values
+    c.bounds.copy_(b)
+    check(c, c.q_h, b, 30, 1, 2)
+    c.close()

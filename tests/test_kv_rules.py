@@ -73,3 +73,11 @@ def test_the_queries_unit_is_a_number(ask):
 def test_queries_whose_unit_overflows_count_as_zero(ask):
     (bits,), (some,) = ask(["unit 1e-37", "unit 4e-37"])
     assert bits == 0 and some != 0
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_select_asks_for_lds_beyond_64_kb(ask, dim):
+    """A block's fixed LDS counts too, and the widest table fits the CU's 160 KB."""
+    sizes = list(range(1, 32768, 97)) + list(range(10900, 12300, 7)) + [11500, 12288, 12289, 32768]
+    for pages, (bytes_, asked) in zip(sizes, ask([f"lds {dim} {n}" for n in sizes])):
+        assert asked == (bytes_ > 64 * 1024) and bytes_ <= 160 * 1024, pages
