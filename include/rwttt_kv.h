@@ -114,7 +114,8 @@ rwttt_status rwttt_kv_destroy(rwttt_kv* kv);
  *                and its position; -1 behind the last one
  *   result       {status, new rows, pages taken, pages returned}
  * Nothing fits in part: with too few pages or a too small cap the status is
- * RWTTT_E_CAPACITY, with a length or ring position out of range it is
+ * RWTTT_E_CAPACITY; with a length or ring position out of range, or more pages
+ * returned than the ring has places beside those it holds, it is
  * RWTTT_E_INVALID; then table and ring stay as they are, lengths is have,
  * new_pos is pos, start and the counts are 0 and the maps -1.
  * Pages returned in a call can be taken by the next one.  Table entries behind

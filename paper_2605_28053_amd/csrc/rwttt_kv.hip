@@ -154,11 +154,9 @@ __global__ void __launch_bounds__(kExtThreads) kv_extend_kernel(const KvExtendLa
     given += y;
     added += z;
   }
-  int code = RWTTT_OK;
-  if (any_bad || front < 0 || front >= pages || count < 0 || count > pages) code = RWTTT_E_INVALID;
-  else if (taken > count || added > p.cap) code = RWTTT_E_CAPACITY;
-  else if (count - taken + given > pages) code = RWTTT_E_INVALID;   // more pages than there are
-  const bool ok = code == RWTTT_OK;
+  const ExtendVerdict verdict = extend_verdict(!any_bad, front, count, pages, taken, given, added, p.cap);
+  const bool ok = verdict == ExtendVerdict::ok;
+  const int code = ok ? RWTTT_OK : verdict == ExtendVerdict::invalid ? RWTTT_E_INVALID : RWTTT_E_CAPACITY;
   if (ok) {
 #pragma unroll
     for (int k = 0; k < TURNS * 4; ++k) {

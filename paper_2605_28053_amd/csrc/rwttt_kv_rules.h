@@ -12,6 +12,23 @@ namespace rwttt {
 constexpr size_t kPlainLds = 64 * 1024;
 
 // ---------------------------------------------------------------------------
+// extend: what a step is refused for
+// ---------------------------------------------------------------------------
+
+enum class ExtendVerdict { ok, invalid, capacity };
+
+// lengths_ok: every length in range.  The ring has room for the pages that come
+// back beside all those it holds: pages taken and pages returned in one call are
+// read and written at once, so the places must not meet.
+constexpr ExtendVerdict extend_verdict(bool lengths_ok, int front, int count, int pages, long long taken,
+                                       long long given, long long added, uint32_t cap) {
+  if (!lengths_ok || front < 0 || front >= pages || count < 0 || count > pages) return ExtendVerdict::invalid;
+  if (taken > count || added > cap) return ExtendVerdict::capacity;
+  if (count + given > pages) return ExtendVerdict::invalid;
+  return ExtendVerdict::ok;
+}
+
+// ---------------------------------------------------------------------------
 // select: which scores are kept
 // ---------------------------------------------------------------------------
 

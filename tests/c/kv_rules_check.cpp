@@ -1,6 +1,8 @@
 // Prints the answers of the paged cache's rules, one line for each query line of stdin:
 //   rank want close n s0 .. s(n-1)   -> the kept indices; bins of at most `close` scores are
 //                                       ranked one by one
+//   extend front count pages taken given added cap -> 0 ok, 1 invalid, 2 capacity, and for a step
+//                                       that is ok the places of the ring both read and written
 //   lds dim max_pages                -> bytes of LDS of a select's block, 1 if they are asked for
 //   unit a                           -> query_unit's bits
 //   cut blocks vh tile longest n l0 .. l(n-1) -> blocks launched, parts, parts of no block, tiles
@@ -97,6 +99,14 @@ int main() {
       std::vector<long long> score(n);
       for (long long& s : score) std::cin >> s;
       rank(want, close, score);
+    } else if (what == "extend") {
+      int front, count, pages, taken, given, added, cap, meet = 0;
+      std::cin >> front >> count >> pages >> taken >> given >> added >> cap;
+      const ExtendVerdict v = extend_verdict(true, front, count, pages, taken, given, added, uint32_t(cap));
+      if (v == ExtendVerdict::ok)
+        for (int i = 0; i < given; ++i)
+          for (int j = 0; j < taken; ++j) meet += (front + count + i) % pages == (front + j) % pages;
+      std::printf("%d %d\n", int(v), meet);
     } else if (what == "lds") {
       int dim, pages;
       std::cin >> dim >> pages;

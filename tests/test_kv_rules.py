@@ -81,3 +81,16 @@ def test_select_asks_for_lds_beyond_64_kb(ask, dim):
     sizes = list(range(1, 32768, 97)) + list(range(10900, 12300, 7)) + [11500, 12288, 12289, 32768]
     for pages, (bytes_, asked) in zip(sizes, ask([f"lds {dim} {n}" for n in sizes])):
         assert asked == (bytes_ > 64 * 1024) and bytes_ <= 160 * 1024, pages
+
+
+def test_extend_never_writes_the_ring_where_it_reads(ask):
+    """Every small ring, and a step that takes and returns pages: it is refused where the
+    returned ones would lie on those that are taken, and only there."""
+    steps = [(front, count, pages, taken, given) for pages in (1, 2, 5, 9) for front in range(pages)
+             for count in range(pages + 1) for taken in range(count + 2) for given in range(pages + 2)]
+    lines = [f"extend {f} {c} {p} {t} {g} 3 3" for f, c, p, t, g in steps]
+    for (front, count, pages, taken, given), (verdict, meet) in zip(steps, ask(lines)):
+        assert meet == 0, (front, count, pages, taken, given)
+        assert verdict == (2 if taken > count else 1 if count + given > pages else 0)
+    assert ask(["extend 0 4 5 1 1 4 3", "extend 5 0 5 0 0 0 0", "extend 0 6 5 0 0 0 0", "extend -1 0 5 0 0 0 0"]) == \
+        [[2, 0], [1, 0], [1, 0], [1, 0]]
