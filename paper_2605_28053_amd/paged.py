@@ -121,9 +121,7 @@ class PagedCache:
         self._rows(q, self.n_heads, "q", self.n_owners)
         if out is None:
             out = torch.full((self.n_owners, self.n_kv_heads, keep), -1, dtype=torch.int32, device=self.device)
-        elif out.dtype != torch.int32 or tuple(out.shape) != (self.n_owners, self.n_kv_heads, keep) \
-                or not out.is_contiguous():
-            raise ValueError("out: contiguous int32 [n_owners, n_kv_heads, keep]")
+        self._dense(out, torch.int32, (self.n_owners, self.n_kv_heads, keep), "out")
         rows = None if rows is None else self._index(rows)
         _check(KV.rwttt_kv_select(
             self.kv, layer, q.data_ptr(), q.stride(0), self.now().data_ptr(), 0 if rows is None else rows.data_ptr(),
@@ -137,12 +135,10 @@ class PagedCache:
         if out is None:
             out = torch.zeros(q.shape, dtype=q.dtype, device=self.device)
         self._rows(out, self.n_heads, "out", self.n_owners)
-        if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (self.n_owners, self.n_heads)
-                                or not lse.is_contiguous()):
-            raise ValueError("lse: contiguous float32 [n_owners, n_heads]")
-        if pages is not None and (pages.dtype != torch.int32 or not pages.is_contiguous()
-                                  or tuple(pages.shape[:2]) != (self.n_owners, self.n_kv_heads)):
-            raise ValueError("pages: contiguous int32 [n_owners, n_kv_heads, keep]")
+        if lse is not None:
+            self._dense(lse, torch.float32, (self.n_owners, self.n_heads), "lse")
+        if pages is not None:
+            self._dense(pages, torch.int32, (self.n_owners, self.n_kv_heads, *pages.shape[-1:]), "pages")
         rows = None if rows is None else self._index(rows)
         _check(KV.rwttt_kv_attend(
             self.kv, layer, q.data_ptr(), q.stride(0), self.now().data_ptr(), 0 if rows is None else rows.data_ptr(),
@@ -170,12 +166,23 @@ class PagedCache:
         return self.new_lengths if self.open else self.lengths
 
     # ---- checks -------------------------------------------------------------
+    def _here(self, t, name):
+        if t.device != self.lengths.device:
+            raise ValueError(f"{name} is on {t.device}, the cache on {self.lengths.device}")
+
+    def _dense(self, t, dtype, shape, name):
+        self._here(t, name)
+        if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+            raise ValueError(f"{name}: contiguous {dtype} {list(shape)}")
+
     def _index(self, t, n=None):
+        self._here(t, "an index array")
         if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or (n is not None and t.numel() != n):
             raise ValueError("index arrays are contiguous int32 vectors" + ("" if n is None else f" of {n}"))
         return t
 
     def _rows(self, t, heads, name, n=None):
+        self._here(t, name)
         if t.dtype != TORCH_DTYPE[self.io_dtype] or t.dim() != 3 or tuple(t.shape[1:]) != (heads, self.head_dim) \
                 or t.stride(2) != 1 or t.stride(1) != self.head_dim or (n is not None and t.shape[0] != n):
             raise ValueError(f"{name}: {self.io_dtype} [{'n' if n is None else n}, {heads}, {self.head_dim}] "

@@ -1,0 +1,63 @@
+"""PagedCache's checks and argument marshalling, on the CPU: the library's calls are recorded,
+not made."""
+
+import pytest
+import torch
+
+pytest.importorskip("paper_2605_28053_amd._rwttt",
+                    reason="librwttt.so not built (python -m paper_2605_28053_amd.build)")
+from paper_2605_28053_amd import paged  # noqa: E402
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    made = []
+    monkeypatch.setattr(paged.KV, "rwttt_kv_create", lambda cfg: 1)
+    monkeypatch.setattr(paged.KV, "rwttt_kv_destroy", lambda kv: 0)
+    for name in ("extend", "append", "select", "attend"):
+        monkeypatch.setattr(paged.KV, "rwttt_kv_" + name, lambda *a, n=name: made.append((n, a)) or 0)
+    monkeypatch.setattr(paged, "_stream", lambda: 0)
+    yield made
+    while caches:                        # their handles are made up
+        caches.pop().kv = None
+
+
+caches = []
+
+
+def cache(heads=4, kv_heads=2, owners=2, **kw):
+    caches.append(paged.PagedCache(owners, 1, heads, kv_heads, 64, n_pages=8, max_pages=4, page_rows=16,
+                                   bound_step=0.05, device="cpu", **kw))
+    return caches[-1]
+
+
+def elsewhere(*shape, dtype=torch.bfloat16):
+    return torch.empty(shape, dtype=dtype, device="meta")
+
+
+def test_tensors_of_another_device_are_refused(calls):
+    """Their addresses would go to the kernels."""
+    c = cache()
+    i32, q, kv = torch.int32, torch.zeros((2, 4, 64), dtype=torch.bfloat16), torch.zeros((2, 2, 64), dtype=torch.bfloat16)
+    rows = torch.zeros(1, dtype=i32)
+    refused = [lambda: c.extend(elsewhere(2, dtype=i32)),
+               lambda: c.attend(0, elsewhere(2, 4, 64)),
+               lambda: c.attend(0, q, out=elsewhere(2, 4, 64)),
+               lambda: c.attend(0, q, lse=elsewhere(2, 4, dtype=torch.float32)),
+               lambda: c.attend(0, q, rows=elsewhere(1, dtype=i32)),
+               lambda: c.attend(0, q, pages=elsewhere(2, 2, 3, dtype=i32)),
+               lambda: c.select(0, elsewhere(2, 4, 64), 3),
+               lambda: c.select(0, q, 3, rows=elsewhere(1, dtype=i32)),
+               lambda: c.select(0, q, 3, out=elsewhere(2, 2, 3, dtype=i32))]
+    for call in refused:
+        with pytest.raises(ValueError):
+            call()
+    c.extend(torch.ones(2, dtype=i32))
+    for k, v in ((elsewhere(2, 2, 64), kv), (kv, elsewhere(2, 2, 64))):
+        with pytest.raises(ValueError):
+            c.append(0, k, v)
+    assert [name for name, _ in calls] == ["extend"]
+    c.append(0, kv, kv)
+    pages = c.select(0, q, 3, rows=rows)
+    c.attend(0, q, pages=pages, rows=rows, lse=torch.zeros((2, 4)))
+    assert [name for name, _ in calls] == ["extend", "append", "select", "attend"]
