@@ -122,11 +122,10 @@ class PagedCache:
         if out is None:
             out = torch.full((self.n_owners, self.n_kv_heads, keep), -1, dtype=torch.int32, device=self.device)
         self._dense(out, torch.int32, (self.n_owners, self.n_kv_heads, keep), "out")
-        rows = None if rows is None else self._index(rows)
+        listed, n = self._listed(rows)
         _check(KV.rwttt_kv_select(
-            self.kv, layer, q.data_ptr(), q.stride(0), self.now().data_ptr(), 0 if rows is None else rows.data_ptr(),
-            self.n_owners if rows is None else rows.numel(), first, last, keep, out.data_ptr(), _stream()),
-            "rwttt_kv_select")
+            self.kv, layer, q.data_ptr(), q.stride(0), self.now().data_ptr(), listed, n, first, last, keep,
+            out.data_ptr(), _stream()), "rwttt_kv_select")
         return out
 
     def attend(self, layer, q, scale=None, window=0, pages=None, rows=None, out=None, lse=None):
@@ -139,11 +138,10 @@ class PagedCache:
             self._dense(lse, torch.float32, (self.n_owners, self.n_heads), "lse")
         if pages is not None:
             self._dense(pages, torch.int32, (self.n_owners, self.n_kv_heads, *pages.shape[-1:]), "pages")
-        rows = None if rows is None else self._index(rows)
+        listed, n = self._listed(rows)
         _check(KV.rwttt_kv_attend(
-            self.kv, layer, q.data_ptr(), q.stride(0), self.now().data_ptr(), 0 if rows is None else rows.data_ptr(),
-            self.n_owners if rows is None else rows.numel(), self.head_dim ** -0.5 if scale is None else scale, window,
-            0 if pages is None else pages.data_ptr(), 0 if pages is None else pages.shape[2], out.data_ptr(),
+            self.kv, layer, q.data_ptr(), q.stride(0), self.now().data_ptr(), listed, n,
+            self.head_dim ** -0.5 if scale is None else scale, window, 0 if pages is None else pages.data_ptr(), 0 if pages is None else pages.shape[2], out.data_ptr(),
             out.stride(0), 0 if lse is None else lse.data_ptr(), _stream()), "rwttt_kv_attend")
         return out
 
@@ -180,6 +178,13 @@ class PagedCache:
         if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or (n is not None and t.numel() != n):
             raise ValueError("index arrays are contiguous int32 vectors" + ("" if n is None else f" of {n}"))
         return t
+
+    def _listed(self, rows):
+        """Address and number of the listed owners; a null address means all of them."""
+        if rows is None:
+            return 0, self.n_owners
+        n = self._index(rows).numel()
+        return rows.data_ptr() if n else self.lengths.data_ptr(), n     # an empty tensor's address is null
 
     def _rows(self, t, heads, name, n=None):
         self._here(t, name)

@@ -61,3 +61,12 @@ def test_tensors_of_another_device_are_refused(calls):
     pages = c.select(0, q, 3, rows=rows)
     c.attend(0, q, pages=pages, rows=rows, lse=torch.zeros((2, 4)))
     assert [name for name, _ in calls] == ["extend", "append", "select", "attend"]
+
+
+def test_an_empty_list_of_owners_computes_none(calls):
+    c = cache()
+    q, none = torch.zeros((2, 4, 64), dtype=torch.bfloat16), torch.zeros(0, dtype=torch.int32)
+    out, pages = torch.full_like(q, 7.0), torch.full((2, 2, 3), 7, dtype=torch.int32)
+    assert c.attend(0, q, rows=none, out=out) is out and c.select(0, q, 3, rows=none, out=pages) is pages
+    for name, args in calls:             # a list of no owners, and not a missing one, which means all of them
+        assert args[5] != 0 and args[6] == 0, name
