@@ -109,40 +109,40 @@ class PagedCache:
         """Store the open step's new rows: k, v [n, n_kv_heads, head_dim], n <= max_new, in slot order."""
         if not self.open:
             raise RuntimeError("append needs an open step: call extend first")
-        self._rows(k, self.n_kv_heads, "k")
-        self._rows(v, self.n_kv_heads, "v")
+        k_stride, v_stride = self._rows(k, self.n_kv_heads, "k"), self._rows(v, self.n_kv_heads, "v")
         if k.shape[0] != v.shape[0] or k.shape[0] > self.max_new:
             raise ValueError("k and v need the same number of rows, max_new at most")
-        _check(KV.rwttt_kv_append(self.kv, layer, k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0),
+        _check(KV.rwttt_kv_append(self.kv, layer, k.data_ptr(), k_stride, v.data_ptr(), v_stride,
                                   self.slots.data_ptr(), k.shape[0], _stream()), "rwttt_kv_append")
 
     def select(self, layer, q, keep, first=1, last=2, rows=None, out=None):
         """Pages [n_owners, n_kv_heads, keep] that each owner's query attends to."""
-        self._rows(q, self.n_heads, "q", self.n_owners)
+        q_stride = self._rows(q, self.n_heads, "q", self.n_owners)
         if out is None:
             out = torch.full((self.n_owners, self.n_kv_heads, keep), -1, dtype=torch.int32, device=self.device)
         self._dense(out, torch.int32, (self.n_owners, self.n_kv_heads, keep), "out")
         listed, n = self._listed(rows)
         _check(KV.rwttt_kv_select(
-            self.kv, layer, q.data_ptr(), q.stride(0), self.now().data_ptr(), listed, n, first, last, keep,
+            self.kv, layer, q.data_ptr(), q_stride, self.now().data_ptr(), listed, n, first, last, keep,
             out.data_ptr(), _stream()), "rwttt_kv_select")
         return out
 
     def attend(self, layer, q, scale=None, window=0, pages=None, rows=None, out=None, lse=None):
         """Attention [n_owners, n_heads, head_dim] of one token q (same shape) per listed owner."""
-        self._rows(q, self.n_heads, "q", self.n_owners)
+        q_stride = self._rows(q, self.n_heads, "q", self.n_owners)
         if out is None:
             out = torch.zeros(q.shape, dtype=q.dtype, device=self.device)
-        self._rows(out, self.n_heads, "out", self.n_owners)
+        out_stride = self._rows(out, self.n_heads, "out", self.n_owners)
         if lse is not None:
             self._dense(lse, torch.float32, (self.n_owners, self.n_heads), "lse")
         if pages is not None:
             self._dense(pages, torch.int32, (self.n_owners, self.n_kv_heads, *pages.shape[-1:]), "pages")
         listed, n = self._listed(rows)
         _check(KV.rwttt_kv_attend(
-            self.kv, layer, q.data_ptr(), q.stride(0), self.now().data_ptr(), listed, n,
-            self.head_dim ** -0.5 if scale is None else scale, window, 0 if pages is None else pages.data_ptr(), 0 if pages is None else pages.shape[2], out.data_ptr(),
-            out.stride(0), 0 if lse is None else lse.data_ptr(), _stream()), "rwttt_kv_attend")
+            self.kv, layer, q.data_ptr(), q_stride, self.now().data_ptr(), listed, n,
+            self.head_dim ** -0.5 if scale is None else scale, window, 0 if pages is None else pages.data_ptr(),
+            0 if pages is None else pages.shape[2], out.data_ptr(), out_stride, 0 if lse is None else lse.data_ptr(),
+            _stream()), "rwttt_kv_attend")
         return out
 
     def commit(self):
@@ -187,11 +187,13 @@ class PagedCache:
         return rows.data_ptr() if n else self.lengths.data_ptr(), n     # an empty tensor's address is null
 
     def _rows(self, t, heads, name, n=None):
+        """Elements between the rows of t [n, heads, head_dim]; a dimension of one may have any stride."""
         self._here(t, name)
-        if t.dtype != TORCH_DTYPE[self.io_dtype] or t.dim() != 3 or tuple(t.shape[1:]) != (heads, self.head_dim) \
-                or t.stride(2) != 1 or t.stride(1) != self.head_dim or (n is not None and t.shape[0] != n):
-            raise ValueError(f"{name}: {self.io_dtype} [{'n' if n is None else n}, {heads}, {self.head_dim}] "
-                             "with dense rows")
+        n = t.shape[0] if n is None and t.dim() else n
+        if t.dtype != TORCH_DTYPE[self.io_dtype] or tuple(t.shape) != (n, heads, self.head_dim) or t.stride(2) != 1 \
+                or (heads > 1 and t.stride(1) != self.head_dim):
+            raise ValueError(f"{name}: {self.io_dtype} [{n}, {heads}, {self.head_dim}] with dense rows")
+        return t.stride(0) if n > 1 else heads * self.head_dim
 
 
 def _stream():

@@ -70,3 +70,21 @@ def test_an_empty_list_of_owners_computes_none(calls):
     assert c.attend(0, q, rows=none, out=out) is out and c.select(0, q, 3, rows=none, out=pages) is pages
     for name, args in calls:             # a list of no owners, and not a missing one, which means all of them
         assert args[5] != 0 and args[6] == 0, name
+
+
+def test_strides_of_dimensions_of_one_do_not_matter(calls):
+    """torch gives a dimension of one any stride: one owner, one new row, one head."""
+    q = torch.zeros((4, 1, 64), dtype=torch.bfloat16).transpose(0, 1)                # [1, 4, 64], stride 64 between rows
+    c = cache(owners=1)
+    c.extend(torch.ones(1, dtype=torch.int32))
+    kv = torch.zeros((2, 1, 64), dtype=torch.bfloat16).transpose(0, 1)
+    c.append(0, kv, kv)
+    c.attend(0, q, out=torch.zeros((4, 1, 64), dtype=torch.bfloat16).transpose(0, 1))
+    c.select(0, q, 3)
+    (_, append), (_, attend), (_, select) = calls[1:]
+    assert append[3] == append[5] == 2 * 64 and attend[3] == attend[13] == select[3] == 4 * 64
+    one = cache(heads=1, kv_heads=1)
+    flat = torch.zeros((2, 3, 64), dtype=torch.bfloat16)[:, 1].unflatten(0, (2, 1))   # [2, 1, 64], rows 192 apart
+    assert flat.shape == (2, 1, 64) and flat.stride(1) != 64
+    one.attend(0, flat)
+    assert calls[-1][1][3] == 192
