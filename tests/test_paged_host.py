@@ -82,7 +82,7 @@ def test_strides_of_dimensions_of_one_do_not_matter(calls):
     c.attend(0, q, out=torch.zeros((4, 1, 64), dtype=torch.bfloat16).transpose(0, 1))
     c.select(0, q, 3)
     (_, append), (_, attend), (_, select) = calls[1:]
-    assert append[3] == append[5] == 2 * 64 and attend[3] == attend[13] == select[3] == 4 * 64
+    assert append[3] == append[5] == 2 * 64 and attend[3] == attend[12] == select[3] == 4 * 64
     one = cache(heads=1, kv_heads=1)
     flat = torch.zeros((2, 3, 64), dtype=torch.bfloat16)[:, 1].unflatten(0, (2, 1))   # [2, 1, 64], rows 192 apart
     assert flat.shape == (2, 1, 64) and flat.stride(1) != 64
