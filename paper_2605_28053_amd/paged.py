@@ -109,6 +109,7 @@ class PagedCache:
         """Store the open step's new rows: k, v [n, n_kv_heads, head_dim], n <= max_new, in slot order."""
         if not self.open:
             raise RuntimeError("append needs an open step: call extend first")
+        self._counts(layer=layer)
         k_stride, v_stride = self._rows(k, self.n_kv_heads, "k"), self._rows(v, self.n_kv_heads, "v")
         if k.shape[0] != v.shape[0] or k.shape[0] > self.max_new:
             raise ValueError("k and v need the same number of rows, max_new at most")
@@ -118,6 +119,7 @@ class PagedCache:
     def select(self, layer, q, keep, first=1, last=2, rows=None, out=None):
         """Pages [n_owners, n_kv_heads, keep] that each owner's query attends to."""
         q_stride = self._rows(q, self.n_heads, "q", self.n_owners)
+        self._counts(layer=layer, keep=keep, first=first, last=last)
         if out is None:
             out = torch.full((self.n_owners, self.n_kv_heads, keep), -1, dtype=torch.int32, device=self.device)
         self._dense(out, torch.int32, (self.n_owners, self.n_kv_heads, keep), "out")
@@ -130,6 +132,7 @@ class PagedCache:
     def attend(self, layer, q, scale=None, window=0, pages=None, rows=None, out=None, lse=None):
         """Attention [n_owners, n_heads, head_dim] of one token q (same shape) per listed owner."""
         q_stride = self._rows(q, self.n_heads, "q", self.n_owners)
+        self._counts(layer=layer, window=window)
         if out is None:
             out = torch.zeros(q.shape, dtype=q.dtype, device=self.device)
         out_stride = self._rows(out, self.n_heads, "out", self.n_owners)
@@ -164,6 +167,12 @@ class PagedCache:
         return self.new_lengths if self.open else self.lengths
 
     # ---- checks -------------------------------------------------------------
+    @staticmethod
+    def _counts(**numbers):
+        for name, x in numbers.items():
+            if not 0 <= x < 1 << 32:     # the binding would wrap it
+                raise ValueError(f"{name} is {x}")
+
     def _here(self, t, name):
         if t.device != self.lengths.device:
             raise ValueError(f"{name} is on {t.device}, the cache on {self.lengths.device}")

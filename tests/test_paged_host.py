@@ -88,3 +88,13 @@ def test_strides_of_dimensions_of_one_do_not_matter(calls):
     assert flat.shape == (2, 1, 64) and flat.stride(1) != 64
     one.attend(0, flat)
     assert calls[-1][1][3] == 192
+
+
+def test_negative_numbers_are_refused(calls):
+    """ctypes would wrap them: a window of -1 meant all rows."""
+    c, q = cache(), torch.zeros((2, 4, 64), dtype=torch.bfloat16)
+    for call in (lambda: c.attend(0, q, window=-1), lambda: c.attend(-1, q), lambda: c.select(0, q, 3, first=-1),
+                 lambda: c.select(0, q, 3, last=-1), lambda: c.select(-1, q, 3), lambda: c.select(0, q, -1)):
+        with pytest.raises((ValueError, RuntimeError)):
+            call()
+    assert calls == []
