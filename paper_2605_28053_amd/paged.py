@@ -117,11 +117,13 @@ class PagedCache:
                                   self.slots.data_ptr(), k.shape[0], _stream()), "rwttt_kv_append")
 
     def select(self, layer, q, keep, first=1, last=2, rows=None, out=None):
-        """Pages [n_owners, n_kv_heads, keep] that each owner's query attends to."""
+        """Pages [n_owners, n_kv_heads, keep] that each listed owner's query attends to; -1 for the others."""
         q_stride = self._rows(q, self.n_heads, "q", self.n_owners)
         self._counts(layer=layer, keep=keep, first=first, last=last)
         if out is None:
-            out = torch.full((self.n_owners, self.n_kv_heads, keep), -1, dtype=torch.int32, device=self.device)
+            shape = (self.n_owners, self.n_kv_heads, keep)
+            out = torch.empty(shape, dtype=torch.int32, device=self.device) if rows is None else \
+                torch.full(shape, -1, dtype=torch.int32, device=self.device)
         self._dense(out, torch.int32, (self.n_owners, self.n_kv_heads, keep), "out")
         listed, n = self._listed(rows)
         _check(KV.rwttt_kv_select(
@@ -130,11 +132,11 @@ class PagedCache:
         return out
 
     def attend(self, layer, q, scale=None, window=0, pages=None, rows=None, out=None, lse=None):
-        """Attention [n_owners, n_heads, head_dim] of one token q (same shape) per listed owner."""
+        """Attention [n_owners, n_heads, head_dim] of one token q (same shape) per listed owner; 0 for the others."""
         q_stride = self._rows(q, self.n_heads, "q", self.n_owners)
         self._counts(layer=layer, window=window)
         if out is None:
-            out = torch.zeros(q.shape, dtype=q.dtype, device=self.device)
+            out = (torch.empty if rows is None else torch.zeros)(q.shape, dtype=q.dtype, device=self.device)
         out_stride = self._rows(out, self.n_heads, "out", self.n_owners)
         if lse is not None:
             self._dense(lse, torch.float32, (self.n_owners, self.n_heads), "lse")

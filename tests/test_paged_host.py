@@ -96,3 +96,13 @@ def test_negative_numbers_are_refused(calls):
         with pytest.raises((ValueError, RuntimeError)):
             call()
     assert calls == []
+
+
+def test_outputs_are_filled_only_where_owners_are_left_out(calls, monkeypatch):
+    """With all owners the kernels write every row: a fill is a launch too many."""
+    c, q, one = cache(), torch.zeros((2, 4, 64), dtype=torch.bfloat16), torch.ones(1, dtype=torch.int32)
+    out, pages = c.attend(0, q, rows=one), c.select(0, q, 3, rows=one)
+    assert bool((out == 0).all()) and bool((pages == -1).all())
+    for name in ("zeros", "full"):
+        monkeypatch.setattr(paged.torch, name, lambda *a, **kw: pytest.fail("filled"))
+    assert c.attend(0, q).shape == q.shape and c.select(0, q, 3).shape == (2, 2, 3)
