@@ -14,6 +14,12 @@ Nothing here waits for the GPU: lengths and slots stay on the device, and
 ``result`` holds the step's status there for whoever wants to read it.  Host
 code only marshals arguments; every number is computed by the library's
 kernels.
+
+``commit`` swaps the buffers of the committed lengths and of the open step's, so
+a graph captures an even number of committed steps: replayed, it goes on from
+where the last replay ended.  Calls go to the current stream, and a cache has
+one workspace: its ``attend`` and ``select`` calls must not overlap in time, so
+calls on several streams need to wait for each other.
 """
 
 import torch

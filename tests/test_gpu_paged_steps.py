@@ -1,4 +1,4 @@
-"""Steps of a PagedCache as a whole."""
+"""Steps of a PagedCache as a whole: rolled back after they took effect, and captured in a graph."""
 
 import pytest
 import torch
@@ -85,3 +85,40 @@ def test_a_step_that_took_effect_is_rolled_back(cache_dtype, kind):
         free = [int(c.ring[(front + i) % 40]) for i in range(count)]
         assert sorted(used + free) == list(range(40))
         c.close()
+
+
+def test_two_captured_steps_replay():
+    """commit swaps two sets of buffers, so a graph holds an even number of steps: replayed,
+    it goes on from where the last replay ended."""
+    def two_steps(c, x):
+        out = []
+        for i in range(2):
+            c.extend(c.lengths + 1)
+            kv = x[i, :, :2 * H].view(R_, 2, H, D)
+            c.append(0, kv[:, 0], kv[:, 1])
+            q = x[i, :, 2 * H:]
+            out.append(c.attend(0, q, pages=c.select(0, q, 4)))
+            c.commit()
+        return out
+
+    x = torch.zeros((2, R_, 2 * H + H * G, D), dtype=torch.bfloat16, device="cuda")
+    eager, graphed = make(max_new=R_), make(max_new=R_)
+    for c in (eager, graphed):
+        two_steps(c, x)                  # the first call of a kernel is not captured
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = two_steps(graphed, x)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    for t in range(50):
+        x.copy_(torch.randn(x.shape, generator=g, device="cuda"))
+        graph.replay()
+        want = two_steps(eager, x)
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a.view(torch.int16), b.view(torch.int16)), t
+        assert graphed.lengths.tolist() == eager.lengths.tolist() == [2 * t + 4] * R_
+        assert torch.equal(graphed.table, eager.table) and torch.equal(graphed.pos, eager.pos)
+    assert graphed.result.tolist()[0] == 0
+    eager.close()
+    graphed.close()
