@@ -68,15 +68,21 @@ class Decoder:
         self.ctx = R.rwttt_create(cfg)
         self.group = R.make_group(R.RWTTT_READ, 0, n_owners)
         self.owners = R.u32_array(range(n_owners))
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)   # the worst of all steps (errors are negative)
 
     def close(self):
         R.rwttt_destroy(self.ctx)
         self.cache.close()
 
+    def extend(self, want):
+        """Open a step of the cache.  One that does not fit leaves the lengths as they are; ``status`` keeps it."""
+        self.cache.extend(want)
+        torch.minimum(self.status, self.cache.result[:1], out=self.status)
+
     def step(self, tokens, want):
         """Logits [n_owners, vocab] of one token per owner; ``want`` are the owners' rows after it."""
         m, n, stream = self.model, self.n_owners, torch.cuda.current_stream().cuda_stream
-        self.cache.extend(want)
+        self.extend(want)
         x = m.embed[tokens]
         for l, w in enumerate(m.layers):
             qkv = (norm(x) @ w["qkv"]).view(n, m.n_heads + 2 * m.n_kv_heads, m.head_dim)
@@ -119,13 +125,13 @@ def main(argv=None):
         over = dec.cache.lengths >= lives
         if bool(over.any()):
             ended += int(over.sum())
-            dec.cache.extend(torch.where(over, 0, dec.cache.lengths))
+            dec.extend(torch.where(over, 0, dec.cache.lengths))
             dec.cache.commit()
         tokens = dec.step(tokens, dec.cache.lengths + 1).argmax(dim=1)
     torch.cuda.synchronize()
     steps = a.steps - a.steps // 10
     took = (time.perf_counter() - begin) / steps
-    code = int(dec.cache.result[0])
+    code = int(dec.status)
     print(f"{a.owners} owners, {a.layers} layers: {took * 1e6:.0f} us a step, {ended} requests ended, "
           f"rows {dec.cache.lengths.tolist()}, free pages {int(dec.cache.pos[1])}, status {code}")
     dec.close()
