@@ -66,7 +66,9 @@ class Decoder:
         self.workspace = torch.empty(R.rwttt_workspace_bytes(cfg), dtype=torch.uint8, device=device)
         cfg.workspace, cfg.workspace_bytes = self.workspace.data_ptr(), self.workspace.numel()
         self.ctx = R.rwttt_create(cfg)
-        self.group = R.make_group(R.RWTTT_READ, 0, n_owners)
+        # one READ takes RWTTT_MAX_GROUP owners at most
+        self.groups = [R.make_group(R.RWTTT_READ, i, min(R.RWTTT_MAX_GROUP, n_owners - i))
+                       for i in range(0, n_owners, R.RWTTT_MAX_GROUP)]
         self.owners = R.u32_array(range(n_owners))
         self.status = torch.zeros(1, dtype=torch.int32, device=device)   # the worst of all steps (errors are negative)
 
@@ -94,9 +96,10 @@ class Decoder:
             gate, up = (norm(x) @ w["up"]).split(m.d_ff, dim=1)
             u = (torch.nn.functional.silu(gate.float()) * up.float()).to(m.dtype)
             y = torch.empty_like(x)
-            st = R.rwttt_read(self.ctx, self.group, self.owners, l, u.data_ptr(), y.data_ptr(), stream)
-            if st != R.RWTTT_OK:
-                raise R.RwtttError(st, "rwttt_read")
+            for group in self.groups:
+                st = R.rwttt_read(self.ctx, group, self.owners, l, u.data_ptr(), y.data_ptr(), stream)
+                if st != R.RWTTT_OK:
+                    raise R.RwtttError(st, "rwttt_read")
             x = x + y
         self.cache.commit()
         return norm(x) @ m.head
