@@ -135,9 +135,12 @@ rwttt_status rwttt_kv_extend(rwttt_kv* kv, const int32_t* have, const int32_t* w
  * 1 / scale and a clamp to +-448.
  * With bounds, the pages' key bounds follow: in units of the head's step, the
  * floor of the least and the ceiling of the largest stored key of each
- * channel, clamped to +-127.  A page whose row 0 is stored forgets its old
- * bounds.  Rows taken back leave bounds wider than they need be, never
- * narrower.  A NaN key leaves its channel's bounds as they are.
+ * channel, the key times 1 / step in fp32, clamped to +-127.  So a stored key is
+ * inside its page's bounds times the step, up to 2^-22 of itself (the product's
+ * rounding), if it is within 127 steps; beyond, the bound is 127 steps and does
+ * not hold it.  A page whose row 0 is stored forgets its old bounds.  Rows taken
+ * back leave bounds wider than they need be, never narrower.  A NaN key leaves
+ * its channel's bounds as they are.
  * The tokens of one page must be consecutive in the call (as rwttt_kv_extend
  * lists them); otherwise which of their bounds remain is not specified.
  * n = 0 launches nothing.  One launch. */
@@ -150,8 +153,9 @@ rwttt_status rwttt_kv_append(rwttt_kv* kv, uint32_t layer, const void* k, uint64
  * the largest scores, `keep` in all (keep >= first + last, keep >= 1); all of
  * them when it has no more than keep.  pages: [n_owners, n_kv_heads, keep],
  * positions in the owner's table row, ascending, -1 behind the last.
- * The score bounds what the page's keys can add to the logits of the head's
- * (rounded) queries together.  With a the largest magnitude in the group's queries and
+ * The score is what the bounds can add to the logits of the head's (rounded)
+ * queries together: no less than the page's keys add, as far as the bounds hold
+ * them (see rwttt_kv_append).  With a the largest magnitude in the group's queries and
  * q8 = rint(q * ((1 / a) * 127)), each step rounded to fp32 (0 for a = 0, or so
  * small, below 3.8e-37, that (1 / a) * 127 overflows),
  *     score = sum over the group's queries and channels of max(q8 lo, q8 hi):
