@@ -176,8 +176,10 @@ rwttt_status rwttt_kv_select(rwttt_kv* kv, uint32_t layer, const void* q, uint64
  * of the listed pages, and then window must be 0.  Of a list only the first
  * min(keep, pages held) entries are read, and -1 or a page that is not held is
  * passed over.  The new token's own row is among the rows once it is appended
- * and counted.  An owner without rows gets out = 0 and lse = -inf; what the
- * pages hold behind an owner's rows, NaN included, has no influence.
+ * and counted.  An owner without rows, a head whose list names none and one
+ * all of whose scores are -inf get out = 0 and lse = -inf.  A score of +inf or
+ * NaN makes the head's out and lse NaN.  What the pages hold behind an owner's
+ * rows, NaN included, has no influence.
  * Products, maxima and sums are held in fp32, out is rounded once.  How a
  * row's sum is split depends on all listed lengths, so its last bits may
  * differ between calls with other lengths; equal calls give equal bits.
