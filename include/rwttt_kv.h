@@ -142,7 +142,8 @@ rwttt_status rwttt_kv_extend(rwttt_kv* kv, const int32_t* have, const int32_t* w
  * back leave bounds wider than they need be, never narrower.  A NaN key leaves
  * its channel's bounds as they are.
  * The tokens of one page must be consecutive in the call (as rwttt_kv_extend
- * lists them); otherwise which of their bounds remain is not specified.
+ * lists them), with no skipped slot between them; otherwise which of their
+ * bounds remain is not specified.
  * n = 0 launches nothing.  One launch. */
 rwttt_status rwttt_kv_append(rwttt_kv* kv, uint32_t layer, const void* k, uint64_t k_stride,
                              const void* v, uint64_t v_stride, const int32_t* slots, uint32_t n,
