@@ -1496,17 +1496,9 @@ hipError_t launch_kv_attend(const KvAttendLaunch& L, hipStream_t stream) {
   p.part = ws.part;
   p.part_ml = ws.part_ml;
   p.scale_log2 = L.scale * 1.4426950408889634f;
-  // What one step reads of all layers at most: above a quarter of the last-level
-  // cache's 256 MB the rest of a step (the owners' fast weights, the projections)
-  // leaves nothing of it for the next one, and the hint keeps it from displacing
-  // what is there (331 against 374 us for 32 owners of 12000-20000 rows, 2.2 GB;
-  // 31.3 against 33.2 us for eight of 4200, 136 MB, where 270 MB of others are read
-  // in between, and 32.4 against 30.8 where only as much is); below, a step finds
-  // the last one's rows there (one owner of 4224, 17 MB: 12.6 against 13.4 us).
   const size_t row_bytes = size_t(L.s.head_dim) * (L.s.cache == RWTTT_F32 ? 4 : L.s.cache == RWTTT_BF16 ? 2 : 1) * 2;
-  const size_t held = size_t(L.s.n_pages), listed = size_t(L.n) * L.keep;
-  const size_t pages = L.pages && listed < held ? listed : held;
-  p.stream = (pages << L.s.page_shift) * row_bytes * L.s.kv_heads * L.n_layers > (size_t(64) << 20);
+  p.stream = attend_streams(L.s.n_pages, L.n, L.s.max_pages, L.keep, L.window, uint64_t(1) << L.s.page_shift,
+                            (row_bytes << L.s.page_shift) * L.s.kv_heads, L.n_layers);
   if (L.s.io_bf16) return L.s.cache == RWTTT_BF16 ? attend_dims<1, RWTTT_BF16>(p, stream)
                                                   : attend_dims<1, RWTTT_FP8>(p, stream);
   return L.s.cache == RWTTT_F32    ? attend_dims<0, RWTTT_F32>(p, stream)

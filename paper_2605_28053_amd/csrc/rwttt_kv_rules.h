@@ -150,6 +150,31 @@ constexpr int attend_grid(uint64_t rows, int longest, int tile, int blocks) {
   return parts_of(rows * row_cost((longest + tile - 1) / tile), blocks);
 }
 
+// Whether the cache's rows are loaded with the non-temporal hint: where one step
+// may read more than a quarter of the last-level cache's 256 MB over all layers.  The
+// rest of a step (the owners' fast weights, the projections) then leaves nothing of
+// them for the next one, and the hint keeps them from displacing what is there.  In
+// us with / without the hint: 331 / 374 for 32 owners of 12000-20000 rows (2.2 GB),
+// 31.3 / 33.2 for eight of 4200 (136 MB) where 270 MB of others are read in between,
+// and 32.4 / 30.8 where only as much is; below, a step finds the last one's rows in
+// the cache: 12.3 / 11.4 for one owner of 4224 (17 MB), 10.9 / 8.9 for eight of 300, 19.8
+// / 17.1 for 32 of 400 (52 MB).
+// The lengths are on the device, so the rule takes the most that the arguments
+// allow: the pool, or what the listed owners can hold, list or have in the window.
+// Short contexts in a large pool get the hint, and lose what the last figures say,
+// if they are all that runs.  A choice on the device, by the lengths, would save
+// them that, but with both loops in one kernel every call takes 0.4 to 0.6 us
+// longer and the largest 337 instead of 332.
+constexpr uint64_t kStreamBytes = uint64_t(64) << 20;
+constexpr bool attend_streams(uint64_t n_pages, uint64_t owners, uint64_t max_pages, uint64_t keep, uint64_t window,
+                              uint64_t page_rows, uint64_t page_bytes, uint64_t layers) {
+  const uint64_t spanned = (window + 2 * page_rows - 2) / page_rows;    // pages that a window can touch
+  uint64_t each = keep ? keep : window ? spanned : max_pages;
+  each = each < max_pages ? each : max_pages;
+  const uint64_t pages = owners * each < n_pages ? owners * each : n_pages;
+  return pages * page_bytes * layers > kStreamBytes;
+}
+
 // A cut that falls in a short row, or near an end of a long one, moves to the
 // row's end: joining costs more than the imbalance (64 owners of up to 300 rows 17.2
 // -> 13.4 us; 24 tiles as the bound of a short row measure the same).

@@ -4,6 +4,7 @@
 //   extend front count pages taken given added cap -> 0 ok, 1 invalid, 2 capacity, and for a step
 //                                       that is ok the places of the ring both read and written
 //   lds dim max_pages                -> bytes of LDS of a select's block, 1 if they are asked for
+//   stream n_pages owners max_pages keep window page_rows page_bytes layers -> 1 if loaded with the hint
 //   unit a                           -> query_unit's bits
 //   cut blocks vh tile longest n l0 .. l(n-1) -> blocks launched, parts, parts of no block, tiles
 //                                       that are not held by one launched part alone, rows whose
@@ -115,6 +116,10 @@ int main() {
                         : dim == 128 ? select_asks_for_lds<128>(pages)
                                      : select_asks_for_lds<256>(pages);
       std::printf("%zu %d\n", fixed + select_lds(pages), asks);
+    } else if (what == "stream") {
+      uint64_t a[8];
+      for (uint64_t& x : a) std::cin >> x;
+      std::printf("%d\n", attend_streams(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7]));
     } else if (what == "unit") {
       std::string text;
       std::cin >> text;

@@ -64,11 +64,11 @@ def test_rows_of_many_columns_are_split_and_joined(io, cache, D, G):
 @pytest.mark.parametrize("io,cache", TYPES)
 @pytest.mark.parametrize("D", [64, 256])
 def test_attend_in_a_large_pool(io, cache, D):
-    """A pool of more than 64 MB, whose rows are loaded with the hint."""
+    """A pool of more than 64 MB, which the owners could hold: its rows are loaded with the hint."""
     H, page, size = 2, 64, {"f32": 4, "bf16": 2, "fp8": 1}[cache]
     extra = (65 << 20) // (2 * H * page * D * size)
     c = Cache([0, 1, 40, 3000, 257, 700], H=H, G=3, D=D, page=page, io=io, cache=cache, seed=D, extra_pages=extra,
-              poison=False)
+              poison=False, max_pages=extra)
     assert 2 * c.N * H * page * D * size > 64 << 20
     got = c.attend()
     for r in range(c.R):

@@ -94,3 +94,17 @@ def test_extend_never_writes_the_ring_where_it_reads(ask):
         assert verdict == (2 if taken > count else 1 if count + given > pages else 0)
     assert ask(["extend 0 4 5 1 1 4 3", "extend 5 0 5 0 0 0 0", "extend 0 6 5 0 0 0 0", "extend -1 0 5 0 0 0 0"]) == \
         [[2, 0], [1, 0], [1, 0], [1, 0]]
+
+
+def test_the_hint_goes_by_the_most_a_call_can_read(ask):
+    """64 KB a page of 16 rows: 1024 pages are 64 MB."""
+    page = 64 << 10
+
+    def hint(n_pages=100000, owners=8, max_pages=1000, keep=0, window=0, rows=16, layers=1):
+        return ask([f"stream {n_pages} {owners} {max_pages} {keep} {window} {rows} {page} {layers}"]) == [[1]]
+    assert hint() and not hint(n_pages=1024) and hint(n_pages=1025)            # the pool
+    assert not hint(max_pages=128) and hint(max_pages=129)                     # what the listed owners can hold
+    assert not hint(owners=1) and hint(owners=2) and hint(owners=1, layers=2)
+    assert not hint(keep=128) and hint(keep=129) and not hint(keep=2000, max_pages=100)
+    # a window of 16 * 127 + 1 rows touches 128 pages where it begins in a page's last row, of 16 * 127 + 2 one more
+    assert not hint(window=16 * 127 + 1) and hint(window=16 * 127 + 2) and hint(window=1 << 23)
