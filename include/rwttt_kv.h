@@ -121,8 +121,9 @@ rwttt_status rwttt_kv_destroy(rwttt_kv* kv);
  * Pages returned in a call can be taken by the next one.  Table entries behind
  * an owner's last page are not cleared.  The inputs stay as they are, so that
  * a call may be repeated; new_pos and lengths must not alias them.
- * Errors of the call itself: RWTTT_E_INVALID for null, misaligned or aliased
- * pointers, or a handle without table or ring.  One launch. */
+ * Errors of the call itself: RWTTT_E_INVALID for null or misaligned pointers,
+ * arrays that overlap (the table and the ring among them; the inputs may be one
+ * another), or a handle without table or ring.  One launch. */
 rwttt_status rwttt_kv_extend(rwttt_kv* kv, const int32_t* have, const int32_t* want,
                              const int32_t* pos, int32_t* new_pos, int32_t* lengths, int32_t* start,
                              int32_t* slots, int32_t* owners, int32_t* positions, uint32_t cap,

@@ -60,6 +60,17 @@ bool layers_ok(void* const* p, uint32_t n) {
   return true;
 }
 
+// An array of an extend.
+struct Ints {
+  const int32_t* p;
+  uint64_t n;
+};
+
+bool overlap(const Ints& a, const Ints& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return x < y ? y - x < a.n * sizeof(int32_t) && b.n != 0 : x - y < b.n * sizeof(int32_t) && a.n != 0;
+}
+
 // A row of `heads` heads and the stride between rows, in elements of the io
 // type: whole 16-byte pieces that do not overlap.
 bool stride_ok(const rwttt_kv* kv, uint64_t stride, uint32_t heads) {
@@ -145,19 +156,22 @@ rwttt_status rwttt_kv_extend(rwttt_kv* kv, const int32_t* have, const int32_t* w
                              int32_t* owners, int32_t* positions, uint32_t cap, int32_t* result,
                              void* stream) {
   if (!kv || !kv->cfg.table || !kv->cfg.ring) return RWTTT_E_INVALID;
-  const void* in[] = {have, want, pos};
-  const void* out[] = {new_pos, lengths, start, result, slots, owners, positions};
-  for (const void* p : in)
-    if (!device16(p)) return RWTTT_E_INVALID;
-  for (int i = 0; i < 7; ++i) {
-    if (i >= 4 && cap == 0 && !out[i]) continue;      // no map entries, no maps
-    if (!device16(out[i])) return RWTTT_E_INVALID;
-    for (const void* p : in)
-      if (p == out[i]) return RWTTT_E_INVALID;
-    for (int j = 0; j < i; ++j)
-      if (out[j] == out[i]) return RWTTT_E_INVALID;
-  }
   if (cap > 0x7fffffffu) return RWTTT_E_INVALID;
+  const uint64_t n = kv->cfg.n_owners;
+  const Ints in[] = {{have, n}, {want, n}, {pos, 2}};
+  const Ints out[] = {{new_pos, 2},     {lengths, n},  {start, n + 1},
+                      {result, 4},      {slots, cap},  {owners, cap},
+                      {positions, cap}, {kv->cfg.table, n * kv->cfg.max_pages}, {kv->cfg.ring, kv->cfg.n_pages}};
+  for (const Ints& a : in)
+    if (!device16(a.p)) return RWTTT_E_INVALID;
+  for (const Ints& a : out) {
+    if (a.n == 0 && !a.p) continue;      // no map entries, no maps
+    if (!device16(a.p)) return RWTTT_E_INVALID;
+    for (const Ints& b : in)
+      if (overlap(a, b)) return RWTTT_E_INVALID;
+    for (const Ints* b = out; b != &a; ++b)
+      if (overlap(a, *b)) return RWTTT_E_INVALID;
+  }
   const rwttt::KvExtendLaunch L{kv->shape, have,  want,  pos,    kv->cfg.table, kv->cfg.ring, new_pos, lengths,
                                 start,     slots, owners, positions, result,      cap};
   return hip_result(kv, rwttt::launch_kv_extend(L, static_cast<hipStream_t>(stream)));
