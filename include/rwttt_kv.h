@@ -12,9 +12,13 @@
  *
  *     rwttt_kv_extend     once: lengths -> pages, table, slots of the new rows
  *     per layer:
+ *       rwttt_kv_rotate   rotary positions of the new queries and keys (rwttt_kv_rows.h)
  *       rwttt_kv_append   new keys and values through the slots
  *       rwttt_kv_select   (long contexts) the pages each query attends to
  *       rwttt_kv_attend   softmax(scale q K^T) V over all, recent or selected rows
+ *
+ * and rwttt_kv_gather (rwttt_kv_rows.h) reads stored rows back, for a prefill over a
+ * prefix or to move an owner.
  *
  * Lengths, tables and slots stay on the device: no call synchronises, copies
  * to the host or depends on a host value that a step changes, so a step can be
@@ -48,8 +52,20 @@
 extern "C" {
 #endif
 
-/* cache element type beside RWTTT_F32 and RWTTT_BF16: OCP e4m3 */
+/* cache element types beside RWTTT_F32 and RWTTT_BF16: OCP e4m3, and OCP e2m1 in
+ * blocks of RWTTT_KV_BLOCK channels that share a power of two (e8m0), 17/32 of a
+ * byte a channel:
+ *
+ *   The pages of a RWTTT_FP4 cache are bytes, [n_pages, n_kv_heads, page_rows *
+ *   head_dim * 17 / 32].  Of a page and head, first the rows' codes, head_dim / 2
+ *   bytes a row, channel 2 i in the low half of byte i; then, for each block of 32
+ *   channels in turn, one byte E a row.  A code is a sign and one of 0, 1/2, 1, 3/2,
+ *   2, 3, 4, 6; its value is that times 2^(E - 127), and NaN for all 32 where E is 255.
+ */
 #define RWTTT_FP8  2
+#define RWTTT_FP4  4
+
+#define RWTTT_KV_BLOCK 32
 
 #define RWTTT_KV_MAX_OWNERS   4096
 #define RWTTT_KV_MAX_ROWS     (1u << 23)   /* largest max_pages * page_rows              */
@@ -67,13 +83,15 @@ typedef struct rwttt_kv_config {
     uint32_t n_kv_heads;     /* 1..512; n_heads / n_kv_heads <= 128               */
     uint32_t head_dim;       /* 64, 128 or 256                                    */
     int32_t  io_dtype;       /* RWTTT_F32 / RWTTT_BF16: q, new keys and values, out */
-    int32_t  cache_dtype;    /* RWTTT_BF16 / RWTTT_FP8, or RWTTT_F32 for fp32 io  */
+    int32_t  cache_dtype;    /* RWTTT_BF16 / RWTTT_FP8 / RWTTT_FP4, or RWTTT_F32 for
+                                fp32 io                                           */
     uint32_t reserved;       /* must be 0                                         */
     /* Device buffers; each may be NULL when no call of the handle needs it. */
     int32_t* table;          /* [n_owners, max_pages] page ids                    */
     int32_t* ring;           /* [n_pages] free pages, a ring                      */
     void* const* k;          /* host array of n_layers pointers to                */
-    void* const* v;          /*   [n_pages, n_kv_heads, page_rows, head_dim]      */
+    void* const* v;          /*   [n_pages, n_kv_heads, page_rows, head_dim], or a
+                                RWTTT_FP4 cache's bytes                           */
     void* const* bounds;     /* host array of n_layers pointers to int8
                                 [n_pages, n_kv_heads, 2, head_dim]: per page and
                                 channel, the least and the largest key           */
@@ -133,7 +151,11 @@ rwttt_status rwttt_kv_extend(rwttt_kv* kv, const int32_t* have, const int32_t* w
  * rows k_stride and v_stride elements apart) in their slots of layer's cache;
  * a slot outside the cache (the -1 of a padded token) is skipped.  Rounded once
  * to the cache type, to nearest even; to RWTTT_FP8 after a product with
- * 1 / scale and a clamp to +-448.
+ * 1 / scale and a clamp to +-448; to RWTTT_FP4 by blocks: with x the exponent of a
+ * block's largest magnitude, one more where its mantissa is 1.75 or above, the
+ * block's E is x - 2 + 127, kept in [2, 252], and a channel's code the nearest to
+ * its value over 2^(E - 127), a tie the even code, what is above 6 the 6.  A block
+ * that holds a NaN or an infinity has E = 255 and reads as NaN.
  * With bounds, the pages' key bounds follow: in units of the head's step, the
  * floor of the least and the ceiling of the largest stored key of each
  * channel, the key times 1 / step in fp32, clamped to +-127.  So a stored key is

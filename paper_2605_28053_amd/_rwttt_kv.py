@@ -1,4 +1,4 @@
-"""ctypes binding of ``include/rwttt_kv.h`` (argument marshalling only).
+"""ctypes binding of ``include/rwttt_kv.h`` and ``include/rwttt_kv_rows.h`` (argument marshalling only).
 
 Every function keeps its C name and returns the C status; device buffers and
 streams are integers (``tensor.data_ptr()``, ``stream.cuda_stream``), 0 for
@@ -10,9 +10,13 @@ import ctypes as C
 from . import _rwttt as R
 
 RWTTT_FP8 = 2
+RWTTT_FP4 = 4
+RWTTT_KV_BLOCK = 32
 RWTTT_KV_MAX_OWNERS = 4096
 RWTTT_KV_MAX_ROWS = 1 << 23
 RWTTT_KV_MAX_SELECT = 32768
+RWTTT_ROTARY_HALF, RWTTT_ROTARY_INTERLEAVED = 0, 1
+RWTTT_ROTARY_PLAIN, RWTTT_ROTARY_LINEAR, RWTTT_ROTARY_BASE, RWTTT_ROTARY_PARTS = 0, 1, 2, 3
 
 
 class rwttt_kv_config(C.Structure):
@@ -26,14 +30,22 @@ class rwttt_kv_config(C.Structure):
                 ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 
+class rwttt_kv_rotary(C.Structure):
+    _fields_ = [("turning", C.c_uint32), ("layout", C.c_int32), ("gain", C.c_float), ("inverse", C.c_int32),
+                ("turns", C.c_void_p)]
+
+
 def _bind(lib):
-    P, U32, U64, I32, VP = C.POINTER, C.c_uint32, C.c_uint64, C.c_int32, C.c_void_p
+    P, U32, U64, I32, VP, F64 = C.POINTER, C.c_uint32, C.c_uint64, C.c_int32, C.c_void_p, C.c_double
     sig = {
         "rwttt_kv_workspace_bytes": (I32, [P(rwttt_kv_config), P(C.c_size_t)]),
         "rwttt_kv_create": (I32, [P(rwttt_kv_config), P(VP)]),
         "rwttt_kv_destroy": (I32, [VP]),
         "rwttt_kv_extend": (I32, [VP] * 10 + [U32, VP, VP]),
         "rwttt_kv_append": (I32, [VP, U32, VP, U64, VP, U64, VP, U32, VP]),
+        "rwttt_kv_gather": (I32, [VP, U32, VP, VP, VP, U32, VP, U64, VP, U64, VP]),
+        "rwttt_kv_turns": (I32, [U32, F64, I32, F64, F64, F64, F64, P(U64)]),
+        "rwttt_kv_rotate": (I32, [VP, P(rwttt_kv_rotary), VP, U32] + [VP, U64] * 4 + [VP]),
         "rwttt_kv_select": (I32, [VP, U32, VP, U64, VP, VP, U32, U32, U32, U32, VP, VP]),
         "rwttt_kv_attend": (I32, [VP, U32, VP, U64, VP, VP, U32, C.c_float, U32, VP, U32, VP, U64, VP, VP]),
         "rwttt_kv_last_hip_error": (I32, [VP]),
@@ -97,6 +109,30 @@ def rwttt_kv_extend(kv, have, want, pos, new_pos, lengths, start, slots, owners,
 
 def rwttt_kv_append(kv, layer, k, k_stride, v, v_stride, slots, n, stream=0):
     return _lib.rwttt_kv_append(kv, layer, k, k_stride, v, v_stride, slots, n, stream)
+
+
+def rwttt_kv_gather(kv, layer, owners, positions, lengths, n, k, k_stride, v, v_stride, stream=0):
+    return _lib.rwttt_kv_gather(kv, layer, owners, positions, lengths, n, k, k_stride, v, v_stride, stream)
+
+
+def rwttt_kv_turns(turning, base, scaling=RWTTT_ROTARY_PLAIN, factor=1.0, low=0.0, high=1.0, context=1.0):
+    """The turning / 2 frequencies in units of 2^-64 turns a position."""
+    out = (C.c_uint64 * max(1, turning // 2))()
+    st = _lib.rwttt_kv_turns(turning, base, scaling, factor, low, high, context, out)
+    if st != R.RWTTT_OK:
+        raise R.RwtttError(st, "rwttt_kv_turns")
+    return list(out)
+
+
+def make_rotary(turning, layout, turns, gain=1.0, inverse=False):
+    """``turns``: address of the frequencies on the device."""
+    return rwttt_kv_rotary(turning, layout, gain, int(inverse), int(turns) or None)
+
+
+def rwttt_kv_rotate(kv, rotary, positions, n, q, q_stride, q_out, q_out_stride, k, k_stride, k_out, k_out_stride,
+                    stream=0):
+    return _lib.rwttt_kv_rotate(kv, C.byref(rotary), positions, n, q, q_stride, q_out, q_out_stride, k, k_stride,
+                                k_out, k_out_stride, stream)
 
 
 def rwttt_kv_select(kv, layer, q, q_stride, lengths, rows, n, first, last, keep, pages, stream=0):

@@ -38,7 +38,7 @@ def _run(cmd):
 def build(verbose=False):
     objdir = os.path.join(PKG, "_build")
     os.makedirs(objdir, exist_ok=True)
-    sources = ("rwttt_kernels.hip", "rwttt_adapter.hip", "rwttt_kv.hip", "rwttt_api.cpp", "rwttt_kv_api.cpp")
+    sources = ("rwttt_kernels.hip", "rwttt_adapter.hip", "rwttt_kv.hip", "rwttt_kv_rows.hip", "rwttt_api.cpp", "rwttt_kv_api.cpp")
     objs = [os.path.join(objdir, os.path.splitext(s)[0] + ".o") for s in sources]
     with ThreadPoolExecutor(len(sources)) as pool:
         list(pool.map(lambda so: _run([HIPCC, "-c", f"--offload-arch={ARCH}", *COMMON, *DEVICE_FLAGS,

@@ -11,6 +11,7 @@ namespace rwttt {
 namespace {
 
 #include "rwttt_device.h"
+#include "rwttt_kv_device.h"
 
 typedef const __attribute__((address_space(4))) int32_t* scalar_i32;   // read through the scalar cache
 
@@ -247,6 +248,7 @@ __device__ __forceinline__ float fp8_clamp(float x) { return x != x ? x : fminf(
 
 template <int IO, int CT> struct AppendRow {   // 16 bytes of io
   static constexpr int E = IO ? 8 : 4;
+  __device__ __forceinline__ void settle() {}
   static constexpr int W = CT == RWTTT_FP8 ? E / 4 : CT == RWTTT_BF16 ? E / 2 : E;   // words in the cache
   uint32_t raw[4];
   __device__ __forceinline__ void load(const char* src) {
@@ -285,9 +287,56 @@ template <int IO, int CT> struct AppendRow {   // 16 bytes of io
   }
 };
 
+// Of a 4-bit cache: the lanes of a block, four of bf16 or eight of fp32, settle its
+// power together; from then on the row holds the values that the cache will (they
+// are numbers of the io type), so that the bounds are those of the stored keys.
+template <int IO> struct AppendRow<IO, RWTTT_FP4> {
+  static constexpr int E = IO ? 8 : 4;
+  uint32_t raw[4], codes, power;
+  __device__ __forceinline__ void load(const char* src) {
+    const u32x4_t t = *reinterpret_cast<const u32x4_t*>(src);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) raw[i] = t[i];
+  }
+  __device__ __forceinline__ float get(int i) const {
+    if constexpr (IO) return i & 1 ? bf16_hi(raw[i / 2]) : bf16_lo(raw[i / 2]);
+    else return __uint_as_float(raw[i]);
+  }
+  __device__ __forceinline__ void settle() {
+    uint32_t top = 0;                    // magnitudes are ordered as their bits are, a NaN's above all
+#pragma unroll
+    for (int i = 0; i < E; ++i) top = max(top, __float_as_uint(get(i)) & 0x7fffffffu);
+    top = max(top, dpp<kDppXor1>(top));
+    top = max(top, dpp<kDppXor2>(top));
+    if constexpr (!IO) top = max(top, dpp<kDppHalfMirror>(top));
+    power = fp4_exponent(top);
+    const float unit = fp4_unit(power == 255u ? 127u : power);
+    codes = 0;
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, get(0), get(1), unit, 0);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, get(2), get(3), unit, 1);
+    if constexpr (IO) {
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, get(4), get(5), unit, 2);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, get(6), get(7), unit, 3);
+      fp4_octet(codes, fp4_unit(power), raw);
+    } else {
+      const f32x2_t a = fp4_floats<0>(codes, fp4_unit(power)), b = fp4_floats<1>(codes, fp4_unit(power));
+      raw[0] = __float_as_uint(a[0]), raw[1] = __float_as_uint(a[1]);
+      raw[2] = __float_as_uint(b[0]), raw[3] = __float_as_uint(b[1]);
+    }
+  }
+  // chunk: of the row's page and head
+  __device__ __forceinline__ void store(char* chunk, int page_rows, int dim, int row, int piece) const {
+    char* dst = chunk + row * (dim / 2) + piece * (E / 2);
+    if constexpr (IO) *reinterpret_cast<uint32_t*>(dst) = codes;
+    else *reinterpret_cast<uint16_t*>(dst) = uint16_t(codes);
+    if (piece % (RWTTT_KV_BLOCK / E) == 0)
+      *reinterpret_cast<uint8_t*>(chunk + fp4_power(page_rows, dim, piece * E / RWTTT_KV_BLOCK, row)) = uint8_t(power);
+  }
+};
+
 // The value of x as the cache holds it.
 template <int CT> __device__ __forceinline__ float stored_value(float x, float scale, float inv_scale) {
-  if constexpr (CT == RWTTT_F32) return x;
+  if constexpr (CT == RWTTT_F32 || CT == RWTTT_FP4) return x;   // a row of 4 bits has settled
   if constexpr (CT == RWTTT_BF16) return bf16_lo(bf16_rne(x));
   return __builtin_amdgcn_cvt_f32_fp8(__builtin_amdgcn_cvt_pk_fp8_f32(fp8_clamp(x * inv_scale), 0.f, 0, false), 0) * scale;
 }
@@ -329,13 +378,29 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const AppendParams ap) {
   if (lane == 0) before = t0 > 0 ? unsigned(p.slots[t0 - 1]) : ~0u;
   const float k_scale = CT == RWTTT_FP8 && p.k_scale ? p.k_scale[h] : 1.f;
   const float v_inv = 1.f / (CT == RWTTT_FP8 && p.v_scale ? p.v_scale[h] : 1.f), k_inv = 1.f / k_scale;
+  if constexpr (CT == RWTTT_FP4) {
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      k[j].settle();
+      v[j].settle();
+    }
+  }
   auto store_rows = [&] {
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
-      const size_t at = ((size_t(slot[j] >> shift) * H + h) * P + (slot[j] & (P - 1))) * size_t(D * CB) + piece * (E * CB);
-      if (slot[j] < rows) {
-        k[j].store(static_cast<char*>(p.k) + at, k_inv);
-        v[j].store(static_cast<char*>(p.v) + at, v_inv);
+      const size_t chunk = size_t(slot[j] >> shift) * H + h;
+      const int row = int(slot[j] & (P - 1));
+      if constexpr (CT == RWTTT_FP4) {
+        if (slot[j] < rows) {
+          k[j].store(static_cast<char*>(p.k) + chunk * fp4_chunk(P, D), P, D, row, piece);
+          v[j].store(static_cast<char*>(p.v) + chunk * fp4_chunk(P, D), P, D, row, piece);
+        }
+      } else {
+        const size_t at = (chunk * P + row) * size_t(D * CB) + piece * (E * CB);
+        if (slot[j] < rows) {
+          k[j].store(static_cast<char*>(p.k) + at, k_inv);
+          v[j].store(static_cast<char*>(p.v) + at, v_inv);
+        }
       }
     }
   };
@@ -345,7 +410,8 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const AppendParams ap) {
   }
 
   // Rounding, scales and step keep the order, so least and largest are found on
-  // the keys as they come in and only these two are rounded.
+  // the keys as they come in and only these two are rounded (rows of 4 bits, each with
+  // its own powers, have settled).
   float lo[E], hi[E];
   auto widen = [&](const Row& r) {
 #pragma unroll
@@ -394,6 +460,8 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const AppendParams ap) {
       Row r[U];
 #pragma unroll
       for (int j = 0; j < U; ++j) r[j].load(src_k + min(u + j * RPI, end - 1) * pitch_k);
+#pragma unroll
+      for (int j = 0; j < U; ++j) r[j].settle();
 #pragma unroll
       for (int j = 0; j < U; ++j) widen(r[j]);   // a row twice changes no bound
     }
@@ -841,12 +909,6 @@ template <int W, bool HINT = false> __device__ __forceinline__ void load_words(c
   }
 }
 
-__device__ __forceinline__ uint32_t fp8_pair(uint32_t w, bool high) {   // exact: e4m3 fits bf16
-  const bf16x2_t h = high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, true)
-                          : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, false);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-
 __device__ __forceinline__ bf16x8_t as_bf16x8(const uint32_t* w) {
   const u32x4_t t = {w[0], w[1], w[2], w[3]};
   return *reinterpret_cast<const bf16x8_t*>(&t);
@@ -885,8 +947,22 @@ template <int CT, int D> struct TileShape {
   static constexpr int VE = D / 16 < KE ? D / 16 : KE, NE = D / 16 / VE, VW = VE * B / 4;
   static constexpr int VR = KT / 4;      // rows of values a lane holds
   static constexpr int NA = D / 16;      // output tiles (four channels a lane)
+  static constexpr int PER = CT == RWTTT_F32 ? 1 : KE / 8;   // operands that a piece of keys feeds
   __device__ static int key_channel(int s, int g) { return (s * 4 + g) * KE; }
   __device__ static int value_channel(int e, int c) { return (e * 16 + c) * VE; }
+};
+
+// Of 4 bits: pieces of 32 channels (16 where a row has no more than 64), a block's or
+// half of one's, and in one lane the D / 16 values of one of a block's channels.
+template <int D> struct TileShape<RWTTT_FP4, D> {
+  static constexpr int KT = tile_rows(RWTTT_FP4), NT = KT / 16;
+  static constexpr int KE = D == 64 ? 16 : 32, KW = D / (4 * KE);
+  static constexpr int VE = D / 16, NE = 1, VW = VE <= 8 ? 1 : VE / 8;
+  static constexpr int VR = KT / 4;
+  static constexpr int NA = D / 16;
+  static constexpr int PER = KE / 8;
+  __device__ static int key_channel(int s, int g) { return (s * 4 + g) * KE; }
+  __device__ static int value_channel(int, int c) { return c * VE; }
 };
 
 // Which pages a tile's halves (16 rows each) lie in, and which of their rows count.
@@ -899,7 +975,7 @@ template <int IO, int CT, int D, bool NT_HINT>
 __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kernel(const AttendParams ap) {
   using S = TileShape<CT, D>;
   constexpr int KT = S::KT, NT = S::NT;
-  constexpr bool F = CT == RWTTT_F32;
+  constexpr bool F = CT == RWTTT_F32, X = CT == RWTTT_FP4;
   constexpr int NQ = IO ? 1 : 3, NP = 3;               // bf16 terms of a query, of a probability
   const KvAttendLaunch& p = ap.L;
   __shared__ uint32_t wave_sum[kAttWaves];
@@ -998,7 +1074,7 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
     };
 
     // queries: the lane's column is one of them; piece s of its channels feeds PER operands
-    constexpr int PER = F ? 1 : S::KE / 8, QN = F ? D / 16 : D / 32, QW = F || IO ? 4 : 8;
+    constexpr int PER = S::PER, QN = F ? D / 16 : D / 32, QW = F || IO ? 4 : 8;
     const char* q_at = static_cast<const char*>(p.q) +
                        (size_t(owner) * p.q_stride + (size_t(h) * G + head0 + (c < heads ? c : 0)) * D) * (IO ? 2 : 4);
     uint32_t qw[QN][QW];
@@ -1017,12 +1093,20 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
 
     uint32_t kw[NT][S::KW][4];
     uint32_t vw[S::NE][S::VR][S::VW];
+    uint32_t kp[X ? NT : 1][X ? S::KW : 1], vp[2];   // 4 bits: powers of the pieces, of the lane's rows
     // row of a half that the lane loads: keys, one a lane; values, VR in turn
     const int k_half = NT == 2 ? c >> 3 : 0, v_half = NT == 2 ? g >> 1 : 0;
     auto half_of = [&](const TileAt<NT>& at, const void* cache, int half) {
       const uint32_t page = NT == 2 && half ? at.page[NT - 1] : at.page[0];
       const int off = NT == 2 && half ? at.off[NT - 1] : at.off[0];
-      return static_cast<const char*>(cache) + ((size_t(page) * H + h) * P + off) * size_t(D * S::B);
+      const size_t chunk = size_t(page) * H + h;
+      if constexpr (X) return static_cast<const char*>(cache) + chunk * fp4_chunk(P, D) + off * (D / 2);
+      else return static_cast<const char*>(cache) + (chunk * P + off) * size_t(D * S::B);
+    };
+    // From a half's first row of 4 bits to the power of its block b.
+    auto power_of = [&](const TileAt<NT>& at, int half, int b) {
+      const int off = NT == 2 && half ? at.off[NT - 1] : at.off[0];
+      return fp4_power(P, D, b, off) - off * (D / 2);
     };
     auto load_keys = [&](const TileAt<NT>& at) {
       const char* src = half_of(at, p.k, k_half);
@@ -1030,11 +1114,29 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
       for (int t = 0; t < NT; ++t) {
         const int rr = NT == 2 ? ((c >> 2) & 1) * 8 + t * 4 + (c & 3) : c;
 #pragma unroll
-        for (int s = 0; s < S::KW; ++s) load_words<4, NT_HINT>(src + (rr * D + S::key_channel(s, g)) * S::B, kw[t][s]);
+        for (int s = 0; s < S::KW; ++s) {
+          if constexpr (X) {
+            load_words<S::KE / 8, NT_HINT>(src + (rr * D + S::key_channel(s, g)) / 2, kw[t][s]);
+            kp[t][s] = *reinterpret_cast<const uint8_t*>(
+                src + power_of(at, k_half, S::key_channel(s, g) / RWTTT_KV_BLOCK) + rr);
+          } else {
+            load_words<4, NT_HINT>(src + (rr * D + S::key_channel(s, g)) * S::B, kw[t][s]);
+          }
+        }
       }
     };
     auto load_values = [&](const TileAt<NT>& at) {
       const char* src = half_of(at, p.v, v_half);
+      if constexpr (X) {
+#pragma unroll
+        for (int k = 0; k < S::VR; ++k) {
+          const char* row = src + (((g & 1) * 8 + k) * D + S::value_channel(0, c)) / 2;
+          if constexpr (D == 64) vw[0][k][0] = *reinterpret_cast<const uint16_t*>(row);
+          else load_words<S::VW, NT_HINT>(row, vw[0][k]);
+        }
+        load_words<2>(src + power_of(at, v_half, S::value_channel(0, c) / RWTTT_KV_BLOCK) + (g & 1) * 8, vp);
+        return;
+      } else {
 #pragma unroll
       for (int e = 0; e < S::NE; ++e)
 #pragma unroll
@@ -1042,6 +1144,7 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
           const int rr = NT == 2 ? (g & 1) * 8 + k : g * 4 + k;
           load_words<S::VW, NT_HINT>(src + (rr * D + S::value_channel(e, c)) * S::B, vw[e][k]);
         }
+      }
     };
 
     TileAt<NT> at = locate(min(t0, seg1 - 1)), next = at;
@@ -1095,6 +1198,10 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
             bf16x8_t key;
             if constexpr (CT == RWTTT_BF16) {
               key = as_bf16x8(kw[k][a]);
+            } else if constexpr (X) {
+              uint32_t wd[4];
+              fp4_octet(kw[k][a / PER][a % PER], fp4_unit(kp[k][a / PER]), wd);
+              key = as_bf16x8(wd);
             } else {
               uint32_t wd[4];
 #pragma unroll
@@ -1147,6 +1254,11 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
           for (int j = 0; j < S::VR; ++j)
 #pragma unroll
             for (int b = 0; b < S::VW; ++b) vw[e][j][b] = j >= from && j < to ? vw[e][j][b] : 0u;
+        if constexpr (X) {               // a power of such a row may be the NaN's
+#pragma unroll
+          for (int j = 0; j < S::VR; ++j)
+            if (j < from || j >= to) vp[j / 4] = (vp[j / 4] & ~(0xffu << (8 * (j % 4)))) | 127u << (8 * (j % 4));
+        }
       }
       if constexpr (F) {
 #pragma unroll
@@ -1160,6 +1272,27 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
       } else {
         bf16x8_t pt[NP];
         split_bf16<NP>(pr, pt);
+        if constexpr (X) {
+          // two rows' pairs of channels, then two channels' pairs of rows
+#pragma unroll
+          for (int a = 0; a < S::VE; a += 2) {
+            uint32_t even[4], odd[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float u0 = fp4_unit(vp[j / 2] >> (16 * (j % 2)) & 0xffu), u1 = fp4_unit(vp[j / 2] >> (16 * (j % 2) + 8) & 0xffu);
+              const uint32_t x = fp4_pair_at(vw[0][2 * j][a / 8], u0, a / 2 % 4);
+              const uint32_t y = fp4_pair_at(vw[0][2 * j + 1][a / 8], u1, a / 2 % 4);
+              even[j] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+              odd[j] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+            }
+            const bf16x8_t v0 = as_bf16x8(even), v1 = as_bf16x8(odd);
+#pragma unroll
+            for (int b = NP - 1; b >= 0; --b) {
+              acc[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pt[b], acc[a], 0, 0, 0);
+              acc[a + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pt[b], acc[a + 1], 0, 0, 0);
+            }
+          }
+        } else {
 #pragma unroll
         for (int e = 0; e < S::NE; ++e)
 #pragma unroll
@@ -1182,6 +1315,7 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
               acc[e * S::VE + a] =
                   __builtin_amdgcn_mfma_f32_16x16x32_bf16(val, pt[b], acc[e * S::VE + a], 0, 0, 0);
           }
+        }
       }
       if (more) {
         load_values(next);
@@ -1442,11 +1576,13 @@ template <int IO, int CT> hipError_t attend_dims(const AttendParams& p, hipStrea
 
 hipError_t launch_kv_append(const KvAppendLaunch& L, hipStream_t stream) {
   const AppendParams p{L, 1};
-  if (L.s.io_bf16) return L.s.cache == RWTTT_BF16 ? append_dims<1, RWTTT_BF16>(p, stream)
-                                                  : append_dims<1, RWTTT_FP8>(p, stream);
+  if (L.s.io_bf16) return L.s.cache == RWTTT_BF16  ? append_dims<1, RWTTT_BF16>(p, stream)
+                          : L.s.cache == RWTTT_FP8 ? append_dims<1, RWTTT_FP8>(p, stream)
+                                                   : append_dims<1, RWTTT_FP4>(p, stream);
   return L.s.cache == RWTTT_F32    ? append_dims<0, RWTTT_F32>(p, stream)
          : L.s.cache == RWTTT_BF16 ? append_dims<0, RWTTT_BF16>(p, stream)
-                                   : append_dims<0, RWTTT_FP8>(p, stream);
+         : L.s.cache == RWTTT_FP8  ? append_dims<0, RWTTT_FP8>(p, stream)
+                                   : append_dims<0, RWTTT_FP4>(p, stream);
 }
 
 hipError_t launch_kv_select(const KvSelectLaunch& L, hipStream_t stream) {
@@ -1496,14 +1632,17 @@ hipError_t launch_kv_attend(const KvAttendLaunch& L, hipStream_t stream) {
   p.part = ws.part;
   p.part_ml = ws.part_ml;
   p.scale_log2 = L.scale * 1.4426950408889634f;
-  const size_t row_bytes = size_t(L.s.head_dim) * (L.s.cache == RWTTT_F32 ? 4 : L.s.cache == RWTTT_BF16 ? 2 : 1) * 2;
+  const size_t bits = L.s.cache == RWTTT_F32 ? 64 : L.s.cache == RWTTT_BF16 ? 32 : L.s.cache == RWTTT_FP8 ? 16 : 8;
+  const size_t row_bytes = size_t(L.s.head_dim) * bits / 8 + (L.s.cache == RWTTT_FP4 ? L.s.head_dim / RWTTT_KV_BLOCK * 2 : 0);
   p.stream = attend_streams(L.s.n_pages, L.n, L.s.max_pages, L.keep, L.window, uint64_t(1) << L.s.page_shift,
                             (row_bytes << L.s.page_shift) * L.s.kv_heads, L.n_layers);
-  if (L.s.io_bf16) return L.s.cache == RWTTT_BF16 ? attend_dims<1, RWTTT_BF16>(p, stream)
-                                                  : attend_dims<1, RWTTT_FP8>(p, stream);
+  if (L.s.io_bf16) return L.s.cache == RWTTT_BF16  ? attend_dims<1, RWTTT_BF16>(p, stream)
+                          : L.s.cache == RWTTT_FP8 ? attend_dims<1, RWTTT_FP8>(p, stream)
+                                                   : attend_dims<1, RWTTT_FP4>(p, stream);
   return L.s.cache == RWTTT_F32    ? attend_dims<0, RWTTT_F32>(p, stream)
          : L.s.cache == RWTTT_BF16 ? attend_dims<0, RWTTT_BF16>(p, stream)
-                                   : attend_dims<0, RWTTT_FP8>(p, stream);
+         : L.s.cache == RWTTT_FP8  ? attend_dims<0, RWTTT_FP8>(p, stream)
+                                   : attend_dims<0, RWTTT_FP4>(p, stream);
 }
 
 }  // namespace rwttt

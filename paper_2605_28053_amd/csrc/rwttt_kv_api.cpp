@@ -1,10 +1,11 @@
 // Host side of the paged key-value cache: the C entry points of
 // include/rwttt_kv.h.  Every argument is checked here, before any launch.
 
+#include <cmath>
 #include <new>
 #include <vector>
 
-#include "rwttt_kv.h"
+#include "rwttt_kv_rows.h"
 #include "rwttt_kv_kernels.h"
 
 struct rwttt_kv {
@@ -31,7 +32,8 @@ rwttt_status check_shape(const rwttt_kv_config* c) {
   if (c->n_heads / c->n_kv_heads > 128) return RWTTT_E_INVALID;
   if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return RWTTT_E_INVALID;
   if (c->io_dtype != RWTTT_F32 && c->io_dtype != RWTTT_BF16) return RWTTT_E_INVALID;
-  if (c->cache_dtype != RWTTT_F32 && c->cache_dtype != RWTTT_BF16 && c->cache_dtype != RWTTT_FP8)
+  if (c->cache_dtype != RWTTT_F32 && c->cache_dtype != RWTTT_BF16 && c->cache_dtype != RWTTT_FP8 &&
+      c->cache_dtype != RWTTT_FP4)
     return RWTTT_E_INVALID;
   if (c->cache_dtype == RWTTT_F32 && c->io_dtype != RWTTT_F32) return RWTTT_E_INVALID;
   return RWTTT_OK;
@@ -76,6 +78,24 @@ bool overlap(const Ints& a, const Ints& b) {
 bool stride_ok(const rwttt_kv* kv, uint64_t stride, uint32_t heads) {
   const uint64_t row = uint64_t(heads) * kv->cfg.head_dim;
   return stride >= row && stride < (uint64_t(1) << 40) && (stride * type_bytes(kv->cfg.io_dtype)) % 16 == 0;
+}
+
+// n rows of queries or keys, elements of the io type.
+struct Rows {
+  const void* p;
+  uint64_t stride, row;
+};
+
+// Whether some of n rows of a are also some of b's; rows side by side within one
+// stride do not meet.
+bool overlap(const Rows& a, const Rows& b, uint64_t n, uint64_t bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  const uint64_t span_a = ((n - 1) * a.stride + a.row) * bytes, span_b = ((n - 1) * b.stride + b.row) * bytes;
+  if (x < y ? y - x >= span_a : x - y >= span_b) return false;
+  if (a.stride != b.stride) return true;
+  const uint64_t step = a.stride * bytes, apart = x < y ? (y - x) % step : (x - y) % step;
+  const uint64_t lower = (x < y ? a.row : b.row) * bytes, upper = (x < y ? b.row : a.row) * bytes;
+  return apart < lower || step - apart < upper;
 }
 
 rwttt_status hip_result(rwttt_kv* kv, hipError_t e) {
@@ -201,6 +221,37 @@ rwttt_status rwttt_kv_append(rwttt_kv* kv, uint32_t layer, const void* k, uint64
   return hip_result(kv, rwttt::launch_kv_append(L, static_cast<hipStream_t>(stream)));
 }
 
+rwttt_status rwttt_kv_gather(rwttt_kv* kv, uint32_t layer, const int32_t* owners, const int32_t* positions,
+                             const int32_t* lengths, uint32_t n, void* k, uint64_t k_stride, void* v,
+                             uint64_t v_stride, void* stream) {
+  if (!kv || layer >= kv->cfg.n_layers || kv->k.empty() || !kv->cfg.table) return RWTTT_E_INVALID;
+  if (n == 0) return RWTTT_OK;
+  if (n > (1u << 24) || !device16(owners) || !device16(positions) || !device16(lengths)) return RWTTT_E_INVALID;
+  if (!k && !v) return RWTTT_E_INVALID;
+  const uint32_t heads = kv->cfg.n_kv_heads;
+  if (k && (misaligned(k, 16) || !stride_ok(kv, k_stride, heads))) return RWTTT_E_INVALID;
+  if (v && (misaligned(v, 16) || !stride_ok(kv, v_stride, heads))) return RWTTT_E_INVALID;
+  const uint64_t row = uint64_t(heads) * kv->cfg.head_dim;
+  if (k && v && overlap(Rows{k, k_stride, row}, Rows{v, v_stride, row}, n, type_bytes(kv->cfg.io_dtype)))
+    return RWTTT_E_INVALID;
+  rwttt::KvGatherLaunch L;
+  L.s = kv->shape;
+  L.k = kv->k[layer];
+  L.v = kv->v[layer];
+  L.k_scale = head_scale(kv, kv->cfg.k_scale, layer);
+  L.v_scale = head_scale(kv, kv->cfg.v_scale, layer);
+  L.table = kv->cfg.table;
+  L.owners = owners;
+  L.positions = positions;
+  L.lengths = lengths;
+  L.n = n;
+  L.k_out = k;
+  L.v_out = v;
+  L.k_stride = k_stride;
+  L.v_stride = v_stride;
+  return hip_result(kv, rwttt::launch_kv_gather(L, static_cast<hipStream_t>(stream)));
+}
+
 rwttt_status rwttt_kv_select(rwttt_kv* kv, uint32_t layer, const void* q, uint64_t q_stride,
                              const int32_t* lengths, const int32_t* rows, uint32_t n, uint32_t first,
                              uint32_t last, uint32_t keep, int32_t* pages, void* stream) {
@@ -251,6 +302,84 @@ rwttt_status rwttt_kv_attend(rwttt_kv* kv, uint32_t layer, const void* q, uint64
   L.lse = lse;
   L.workspace = kv->cfg.workspace;
   return hip_result(kv, rwttt::launch_kv_attend(L, static_cast<hipStream_t>(stream)));
+}
+
+rwttt_status rwttt_kv_turns(uint32_t turning, double base, int32_t scaling, double factor, double low, double high,
+                            double context, uint64_t* turns) {
+  if (!turns || turning == 0 || turning % 2 || !std::isfinite(base) || base <= 1.0) return RWTTT_E_INVALID;
+  if (scaling < RWTTT_ROTARY_PLAIN || scaling > RWTTT_ROTARY_PARTS) return RWTTT_E_INVALID;
+  if (scaling != RWTTT_ROTARY_PLAIN && (!std::isfinite(factor) || factor <= 0.0)) return RWTTT_E_INVALID;
+  if (scaling == RWTTT_ROTARY_BASE && turning == 2) return RWTTT_E_INVALID;
+  if (scaling == RWTTT_ROTARY_PARTS && (!std::isfinite(low) || !std::isfinite(high) || !std::isfinite(context) ||
+                                        context <= 0.0 || high <= low))
+    return RWTTT_E_INVALID;
+  // long double: 64 bits of mantissa, as many as a turn is divided into
+  const long double two_pi = 6.283185307179586476925286766559005768L, d = turning, f = factor;
+  const long double b = scaling == RWTTT_ROTARY_BASE ? base * powl(f, d / (d - 2)) : static_cast<long double>(base);
+  for (uint32_t i = 0; i < turning / 2; ++i) {
+    long double t = powl(b, -2.0L * i / d) / two_pi;            // turns a position
+    if (scaling == RWTTT_ROTARY_LINEAR) t /= f;
+    if (scaling == RWTTT_ROTARY_PARTS) {
+      long double r = (context * t - low) / (static_cast<long double>(high) - low);
+      r = r < 0 ? 0 : r > 1 ? 1 : r;
+      t = t * (r + (1 - r) / f);
+    }
+    t -= floorl(t);                                             // whole turns do not count
+    const long double units = rintl(ldexpl(t, 64));
+    turns[i] = units >= 0x1p64L ? 0 : static_cast<uint64_t>(units);
+  }
+  return RWTTT_OK;
+}
+
+rwttt_status rwttt_kv_rotate(rwttt_kv* kv, const rwttt_kv_rotary* rotary, const int32_t* positions, uint32_t n,
+                             const void* q, uint64_t q_stride, void* q_out, uint64_t q_out_stride, const void* k,
+                             uint64_t k_stride, void* k_out, uint64_t k_out_stride, void* stream) {
+  if (!kv || !rotary) return RWTTT_E_INVALID;
+  const rwttt_kv_config& c = kv->cfg;
+  if (rotary->turning == 0 || rotary->turning % 2 || rotary->turning > c.head_dim) return RWTTT_E_INVALID;
+  if (rotary->layout != RWTTT_ROTARY_HALF && rotary->layout != RWTTT_ROTARY_INTERLEAVED) return RWTTT_E_INVALID;
+  if (!std::isfinite(rotary->gain) || (rotary->inverse != 0 && rotary->inverse != 1) || !device16(rotary->turns))
+    return RWTTT_E_INVALID;
+  if (n == 0) return RWTTT_OK;
+  if (n > (1u << 24) || !device16(positions) || (!q && !k)) return RWTTT_E_INVALID;
+  const uint64_t bytes = type_bytes(c.io_dtype);
+  struct Side {
+    const void* in;
+    uint64_t stride;
+    void* out;
+    uint64_t out_stride;
+    uint32_t heads;
+  };
+  const Side sides[] = {{q, q_stride, q_out, q_out_stride, c.n_heads}, {k, k_stride, k_out, k_out_stride, c.n_kv_heads}};
+  for (const Side& a : sides) {
+    if ((a.in == nullptr) != (a.out == nullptr)) return RWTTT_E_INVALID;
+    if (!a.in) continue;
+    if (misaligned(a.in, 16) || misaligned(a.out, 16) || !stride_ok(kv, a.stride, a.heads) ||
+        !stride_ok(kv, a.out_stride, a.heads))
+      return RWTTT_E_INVALID;
+  }
+  for (const Side& a : sides)
+    for (const Side& b : sides) {
+      if (!a.in || !b.in) continue;
+      const uint64_t row_a = uint64_t(a.heads) * c.head_dim, row_b = uint64_t(b.heads) * c.head_dim;
+      const Rows out{a.out, a.out_stride, row_a};
+      const bool itself = &a == &b && a.in == a.out && a.stride == a.out_stride;
+      if (!itself && overlap(out, Rows{b.in, b.stride, row_b}, n, bytes)) return RWTTT_E_INVALID;
+      if (&a != &b && overlap(out, Rows{b.out, b.out_stride, row_b}, n, bytes)) return RWTTT_E_INVALID;
+    }
+  rwttt::KvRotateLaunch L;
+  L.io_bf16 = kv->shape.io_bf16;
+  L.head_dim = kv->shape.head_dim;
+  L.turning = int(rotary->turning);
+  L.interleaved = rotary->layout == RWTTT_ROTARY_INTERLEAVED;
+  L.inverse = rotary->inverse;
+  L.gain = rotary->gain;
+  L.turns = rotary->turns;
+  L.positions = positions;
+  L.n = n;
+  L.q = {q, q_out, q_stride, q_out_stride, q ? int(c.n_heads) : 0};
+  L.k = {k, k_out, k_stride, k_out_stride, k ? int(c.n_kv_heads) : 0};
+  return hip_result(kv, rwttt::launch_kv_rotate(L, static_cast<hipStream_t>(stream)));
 }
 
 int32_t rwttt_kv_last_hip_error(const rwttt_kv* kv) { return kv ? kv->last_hip : 0; }

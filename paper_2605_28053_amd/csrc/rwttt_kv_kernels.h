@@ -6,14 +6,14 @@
 #include <stddef.h>
 #include <stdint.h>
 
-#include "rwttt_kv.h"
+#include "rwttt_kv_rows.h"
 
 namespace rwttt {
 
 // Shape of a handle's cache.
 struct KvShape {
   int n_owners, n_pages, page_shift, max_pages, kv_heads, group, head_dim;
-  int io_bf16, cache;      // cache: RWTTT_F32, RWTTT_BF16 or RWTTT_FP8
+  int io_bf16, cache;      // cache: RWTTT_F32, RWTTT_BF16, RWTTT_FP8 or RWTTT_FP4
 };
 
 struct KvExtendLaunch {
@@ -32,6 +32,33 @@ struct KvAppendLaunch {
   const float *k_scale, *v_scale, *step;    // of the layer; scales may be null
   const int32_t* slots;
   uint32_t n;
+};
+
+struct KvGatherLaunch {
+  KvShape s;
+  const void *k, *v;                        // of the layer
+  const float *k_scale, *v_scale;           // of the layer, may be null
+  const int32_t *table, *owners, *positions, *lengths;
+  uint32_t n;
+  void *k_out, *v_out;                      // one of them may be null
+  uint64_t k_stride, v_stride;
+};
+
+// One side of a rotation: the rows of `heads` heads of n tokens, and where they go.
+struct KvTurnRows {
+  const void* in;
+  void* out;
+  uint64_t in_stride, out_stride;
+  int heads;                                // 0: no such side
+};
+
+struct KvRotateLaunch {
+  int io_bf16, head_dim, turning, interleaved, inverse;
+  float gain;
+  const uint64_t* turns;
+  const int32_t* positions;
+  uint32_t n;
+  KvTurnRows q, k;
 };
 
 struct KvSelectLaunch {
@@ -61,6 +88,8 @@ struct KvAttendLaunch {
 size_t kv_workspace_bytes(const KvShape& shape);
 hipError_t launch_kv_extend(const KvExtendLaunch& L, hipStream_t stream);
 hipError_t launch_kv_append(const KvAppendLaunch& L, hipStream_t stream);
+hipError_t launch_kv_gather(const KvGatherLaunch& L, hipStream_t stream);
+hipError_t launch_kv_rotate(const KvRotateLaunch& L, hipStream_t stream);
 hipError_t launch_kv_select(const KvSelectLaunch& L, hipStream_t stream);
 hipError_t launch_kv_attend(const KvAttendLaunch& L, hipStream_t stream);
 

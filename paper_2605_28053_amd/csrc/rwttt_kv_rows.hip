@@ -1,0 +1,261 @@
+// Kernels of the operators on rows (include/rwttt_kv_rows.h) for gfx950: rotary
+// positions, and stored rows read back.
+
+#include "rwttt_kv_kernels.h"
+
+#include <type_traits>
+
+namespace rwttt {
+namespace {
+
+#include "rwttt_device.h"
+#include "rwttt_kv_device.h"
+
+// ---------------------------------------------------------------------------
+// rotate: rotary positions
+// ---------------------------------------------------------------------------
+//
+// An angle in turns is position * frequency, both whole numbers (the frequency
+// times 2^64), so the product modulo 2^64 is the exact place within a turn, at
+// position 1 as at 2^31; taken as a signed number, its conversion to fp32 keeps
+// 24 bits of small angles as well.
+//
+// A block takes some tokens, computes their sines and cosines once into LDS --
+// heads share them -- and passes over its part of the rows.  A lane owns whole
+// pairs, so a row may be turned in place: with HALF 16 bytes of each partner, with
+// INTERLEAVED 16 bytes.  Where a half of the turning channels is no whole number
+// of 16 bytes, a lane owns one pair.
+
+constexpr int kRotThreads = 256;
+
+template <int IO> struct IoRow {           // 16 bytes of io
+  static constexpr int E = IO ? 8 : 4;
+  uint32_t w[4];
+  __device__ __forceinline__ void load(const char* p) {
+    const u32x4_t t = *reinterpret_cast<const u32x4_t*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = t[i];
+  }
+  __device__ __forceinline__ void store(char* p) const {
+    *reinterpret_cast<u32x4_t*>(p) = (u32x4_t){w[0], w[1], w[2], w[3]};
+  }
+  __device__ __forceinline__ float get(int i) const {
+    if constexpr (IO) return i & 1 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]);
+    else return __uint_as_float(w[i]);
+  }
+  __device__ __forceinline__ void put_pair(int i, float a, float b) {   // elements 2 i, 2 i + 1
+    if constexpr (IO) w[i] = bf16x2_rne(a, b);
+    else {
+      w[2 * i] = __float_as_uint(a);
+      w[2 * i + 1] = __float_as_uint(b);
+    }
+  }
+};
+
+struct RotateParams {
+  KvRotateLaunch L;
+  int tokens;              // of a block
+  int units;               // of a head: what one lane takes at a time
+  int per_token, part;     // units of a token, of a block's part of them
+};
+
+// How the units of a head are laid out.
+enum class Turn { half, interleaved, pairs };   // pairs: HALF, one pair a unit
+
+__device__ __forceinline__ float2 turned(float2 x, float2 cs) {
+  return make_float2(fmaf(x.x, cs.x, -(x.y * cs.y)), fmaf(x.y, cs.x, x.x * cs.y));
+}
+
+template <int IO, Turn T>
+__global__ void __launch_bounds__(kRotThreads) kv_rotate_kernel(const RotateParams rp) {
+  const KvRotateLaunch& p = rp.L;
+  constexpr int B = IO ? 2 : 4, E = IoRow<IO>::E;
+  extern __shared__ float2 cs[];         // [tokens][turning / 2]: gain cos, gain sin
+  const int half = p.turning / 2, n = int(p.n);
+  const int t0 = blockIdx.x * rp.tokens, nt = min(rp.tokens, n - t0);
+  const int u0 = blockIdx.y * rp.part, u1 = min(rp.per_token, u0 + rp.part);
+
+  for (int i = threadIdx.x; i < nt * half; i += kRotThreads) {
+    const int pos = p.positions[t0 + i / half];
+    const int64_t place = int64_t(uint64_t(uint32_t(pos)) * p.turns[i % half]);
+    float s, c;
+    sincospif(float(place) * 0x1p-63f, &s, &c);
+    cs[i] = make_float2(c * p.gain, (p.inverse ? -s : s) * p.gain);
+  }
+  __syncthreads();
+
+  const int span = u1 - u0;
+  for (int i = threadIdx.x; i < nt * span; i += kRotThreads) {
+    const int t = i / span, u = u0 + i % span;
+    if (p.positions[t0 + t] < 0) continue;
+    int h = u / rp.units;
+    const int x = u % rp.units;
+    const bool is_k = h >= p.q.heads;
+    const KvTurnRows& rows = is_k ? p.k : p.q;
+    h -= is_k ? p.q.heads : 0;
+    const char* src = static_cast<const char*>(rows.in) + ((t0 + t) * rows.in_stride + size_t(h) * p.head_dim) * B;
+    char* dst = static_cast<char*>(rows.out) + ((t0 + t) * rows.out_stride + size_t(h) * p.head_dim) * B;
+    const float2* at = cs + t * half;
+    if constexpr (T == Turn::half) {
+      const int pairs = half / E;
+      if (x < pairs) {
+        IoRow<IO> a, b;
+        a.load(src + x * 16);
+        b.load(src + half * B + x * 16);
+        IoRow<IO> ra, rb;
+#pragma unroll
+        for (int j = 0; j < E; j += 2) {
+          const float2 y0 = turned(make_float2(a.get(j), b.get(j)), at[x * E + j]);
+          const float2 y1 = turned(make_float2(a.get(j + 1), b.get(j + 1)), at[x * E + j + 1]);
+          ra.put_pair(j / 2, y0.x, y1.x);
+          rb.put_pair(j / 2, y0.y, y1.y);
+        }
+        ra.store(dst + x * 16);
+        rb.store(dst + half * B + x * 16);
+      } else {
+        IoRow<IO> a;
+        a.load(src + (x + pairs) * 16);
+        a.store(dst + (x + pairs) * 16);
+      }
+    } else if constexpr (T == Turn::interleaved) {
+      IoRow<IO> a, r;
+      a.load(src + x * 16);
+      r = a;
+#pragma unroll
+      for (int j = 0; j < E / 2; ++j) {
+        const int k = x * (E / 2) + j;
+        if (k < half) {
+          const float2 y = turned(make_float2(a.get(2 * j), a.get(2 * j + 1)), at[k]);
+          r.put_pair(j, y.x, y.y);
+        }
+      }
+      r.store(dst + x * 16);
+    } else {
+      using M = Elem<std::conditional_t<IO, uint16_t, float>>;
+      if (x < half) {
+        const float2 y = turned(make_float2(M::get(src, x), M::get(src, x + half)), at[x]);
+        M::put(dst, x, y.x);
+        M::put(dst, x + half, y.y);
+      } else {
+        M::put(dst, x + half, M::get(src, x + half));
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// gather: stored rows read back
+// ---------------------------------------------------------------------------
+//
+// A wave takes one kv head of a run of rows: LPR lanes hold a row, 16 bytes of
+// output each, and the loads of its keys and values are in flight at once behind
+// the chain owner -> length and page.
+
+struct GatherParams {
+  KvGatherLaunch L;
+  int run;               // rows a wave takes
+};
+
+template <int IO, int CT, int D, int NI>
+__global__ void __launch_bounds__(256) kv_gather_kernel(const GatherParams gp) {
+  const KvGatherLaunch& p = gp.L;
+  using Row = CachedRow<IO, CT, D>;
+  constexpr int IOB = IO ? 2 : 4, E = Row::E, LPR = D / E, RPI = 64 / LPR;
+  const int lane = threadIdx.x & 63, unit = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int H = p.s.kv_heads, shift = p.s.page_shift, P = 1 << shift;
+  const int h = unit % H, n = int(p.n), t0 = unit / H * gp.run, t1 = min(n, t0 + gp.run);
+  if (t0 >= n) return;
+  const int sub = lane / LPR, piece = lane % LPR, most = p.s.max_pages << shift;
+
+  int page[NI], row[NI];                 // page -1: skipped
+#pragma unroll
+  for (int j = 0; j < NI; ++j) {
+    const int t = t0 + j * RPI + sub, at = min(t, t1 - 1);
+    const int owner = p.owners[at], pos = p.positions[at];
+    const bool there = t < t1 && unsigned(owner) < unsigned(p.s.n_owners);
+    const int r = there ? owner : 0;
+    const bool held = there && pos >= 0 && pos < min(p.lengths[r], most);
+    const int entry = p.table[size_t(r) * p.s.max_pages + (held ? pos >> shift : 0)];
+    page[j] = held ? int(min(uint32_t(entry), uint32_t(p.s.n_pages - 1))) : -1;
+    row[j] = held ? pos & (P - 1) : 0;
+  }
+  Row k[NI], v[NI];
+#pragma unroll
+  for (int j = 0; j < NI; ++j) {
+    const size_t chunk = size_t(max(page[j], 0)) * H + h;
+    if (p.k_out) k[j].load(static_cast<const char*>(p.k), chunk, P, row[j], piece);
+    if (p.v_out) v[j].load(static_cast<const char*>(p.v), chunk, P, row[j], piece);
+  }
+  const float ks = CT == RWTTT_FP8 && p.k_scale ? p.k_scale[h] : 1.f;
+  const float vs = CT == RWTTT_FP8 && p.v_scale ? p.v_scale[h] : 1.f;
+#pragma unroll
+  for (int j = 0; j < NI; ++j) {
+    const size_t t = size_t(t0 + j * RPI + sub);
+    if (page[j] >= 0) {
+      const size_t col = size_t(h) * D * IOB + piece * 16;
+      if (p.k_out) k[j].store(static_cast<char*>(p.k_out) + t * p.k_stride * IOB + col, ks);
+      if (p.v_out) v[j].store(static_cast<char*>(p.v_out) + t * p.v_stride * IOB + col, vs);
+    }
+  }
+}
+
+template <int IO, int CT, int D> hipError_t gather_go(GatherParams p, hipStream_t stream) {
+  constexpr int RPI = 64 * (IO ? 8 : 4) / D;
+  const uint64_t rows = uint64_t(p.L.n) * p.L.s.kv_heads;
+  const bool many = rows >= 4096u * 4 * RPI;
+  p.run = many ? 4 * RPI : RPI;
+  const uint64_t units = uint64_t((p.L.n + p.run - 1) / p.run) * p.L.s.kv_heads;
+  const dim3 grid(unsigned((units + 3) / 4)), block(256);
+  if (many) hipLaunchKernelGGL((kv_gather_kernel<IO, CT, D, 4>), grid, block, 0, stream, p);
+  else hipLaunchKernelGGL((kv_gather_kernel<IO, CT, D, 1>), grid, block, 0, stream, p);
+  return hipGetLastError();
+}
+
+template <int IO, int CT> hipError_t gather_dims(const GatherParams& p, hipStream_t stream) {
+  return p.L.s.head_dim == 64    ? gather_go<IO, CT, 64>(p, stream)
+         : p.L.s.head_dim == 128 ? gather_go<IO, CT, 128>(p, stream)
+                                 : gather_go<IO, CT, 256>(p, stream);
+}
+
+template <int IO> hipError_t rotate_go(const RotateParams& p, Turn how, dim3 grid, size_t lds, hipStream_t stream) {
+  auto kernel = how == Turn::half          ? kv_rotate_kernel<IO, Turn::half>
+                : how == Turn::interleaved ? kv_rotate_kernel<IO, Turn::interleaved>
+                                           : kv_rotate_kernel<IO, Turn::pairs>;
+  hipLaunchKernelGGL(kernel, grid, dim3(kRotThreads), lds, stream, p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_kv_gather(const KvGatherLaunch& L, hipStream_t stream) {
+  const GatherParams p{L, 1};
+  if (L.s.io_bf16) return L.s.cache == RWTTT_BF16  ? gather_dims<1, RWTTT_BF16>(p, stream)
+                          : L.s.cache == RWTTT_FP8 ? gather_dims<1, RWTTT_FP8>(p, stream)
+                                                   : gather_dims<1, RWTTT_FP4>(p, stream);
+  return L.s.cache == RWTTT_F32    ? gather_dims<0, RWTTT_F32>(p, stream)
+         : L.s.cache == RWTTT_BF16 ? gather_dims<0, RWTTT_BF16>(p, stream)
+         : L.s.cache == RWTTT_FP8  ? gather_dims<0, RWTTT_FP8>(p, stream)
+                                   : gather_dims<0, RWTTT_FP4>(p, stream);
+}
+
+hipError_t launch_kv_rotate(const KvRotateLaunch& L, hipStream_t stream) {
+  RotateParams p;
+  p.L = L;
+  const int E = L.io_bf16 ? 8 : 4, half = L.turning / 2;
+  const Turn how = L.interleaved ? Turn::interleaved : half % E == 0 ? Turn::half : Turn::pairs;
+  const bool in_place = (!L.q.heads || L.q.in == L.q.out) && (!L.k.heads || L.k.in == L.k.out);
+  // in place the channels that do not turn are where they belong
+  const int rest = in_place ? 0 : L.head_dim - L.turning;
+  p.units = how == Turn::half          ? half / E + rest / E
+            : how == Turn::interleaved ? ((in_place ? L.turning : L.head_dim) + E - 1) / E
+                                       : half + rest;
+  p.per_token = p.units * (L.q.heads + L.k.heads);
+  p.tokens = 1;
+  p.part = p.per_token > 1024 * kRotThreads ? (p.per_token + 1023) / 1024 : kRotThreads;
+  const unsigned blocks = (L.n + p.tokens - 1) / p.tokens, parts = unsigned((p.per_token + p.part - 1) / p.part);
+  const dim3 grid(blocks, parts);
+  const size_t lds = size_t(p.tokens) * half * sizeof(float2);
+  return L.io_bf16 ? rotate_go<1>(p, how, grid, lds, stream) : rotate_go<0>(p, how, grid, lds, stream);
+}
+
+}  // namespace rwttt

@@ -1,0 +1,388 @@
+"""The 4-bit paged cache on the GPU: rows as they are stored, read back and attended to."""
+
+import math
+import random
+
+import pytest
+import torch
+
+from paper_2605_28053_amd import _rwttt_kv as KV
+from tests.kv4_util import BLOCK, Cache4, decode_ref, encode_ref, gather, stored4, unpack
+from tests.kv_util import DT, Cache, bounds_ref, dev, i32, ok, pages_of, select_ref, stream
+
+pytestmark = pytest.mark.gpu
+
+EDGES = [0, 1, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 130, 0, 257]
+
+
+# ---------------------------------------------------------------------------
+# append and gather
+# ---------------------------------------------------------------------------
+
+def append(c, k, v, slots, strided=False):
+    """Stores rows k, v [n, H, D] (CPU, io type) and returns the caches' bytes."""
+    n = k.shape[0]
+    if strided:
+        both = torch.cat([k, v], dim=1).cuda()
+        kd, vd = both[:, :c.H], both[:, c.H:]
+    else:
+        kd, vd = dev(k), dev(v)
+    ok(KV.rwttt_kv_append(c.kv, 0, kd.data_ptr(), kd.stride(0), vd.data_ptr(), vd.stride(0), i32(slots).data_ptr(), n, stream()))
+    torch.cuda.synchronize()
+    return c.kd.cpu(), c.vd.cpu()
+
+
+def after(c, x, rows, slots):
+    """The bytes that the cache x should hold after an append."""
+    code, E = c.code[x].clone(), c.E[x].clone()
+    cr, er = encode_ref(rows)
+    for t, s in enumerate(slots):
+        if 0 <= s < c.N * c.page:
+            code[s // c.page, :, s % c.page], E[s // c.page, :, s % c.page] = cr[t], er[t]
+    return code, E
+
+
+def same_bytes(raw, code, E, P, D):
+    got_code, got_E = unpack(raw, P, D)
+    assert torch.equal(got_E, E)
+    nan = (E == 255).repeat_interleave(BLOCK, dim=-1)            # the codes of a block that reads as NaN say nothing
+    assert torch.equal(torch.where(nan, 0, got_code), torch.where(nan, 0, code))
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("page", [16, 128])
+def test_rows_are_stored_by_the_book(io, D, page):
+    """Magnitudes over 60 powers of two, blocks of zeros, odd heads, a stride, skipped slots."""
+    g = torch.Generator().manual_seed(D + page)
+    c = Cache4([40, 3], H=3, G=1, D=D, page=page, io=io, seed=1, extra_pages=4)
+    n = 37
+    size = torch.exp2(torch.randint(-30, 30, (n, 3, D // BLOCK, 1), generator=g).float())
+    k, v = ((torch.randn((n, 3, D // BLOCK, BLOCK), generator=g) * size).flatten(-2) for _ in range(2))
+    k[5], v[6, 1, :BLOCK] = 0.0, -0.0
+    k, v = k.to(DT[io]), v.to(DT[io])
+    slots = random.Random(D).sample(range(c.N * page), n)
+    slots[3], slots[9], slots[36] = -1, c.N * page, -7
+    raw = append(c, k, v, slots, strided=True)
+    for x, rows, got in zip("kv", (k, v), raw):
+        same_bytes(got, *after(c, x, rows, slots), page, D)
+    c.close()
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_ties_borders_and_what_is_not_finite(io):
+    """Every border of the grid and its neighbours, at powers from the least to the most; largest
+    magnitudes about the mantissa where the power steps; subnormals; infinities and NaN."""
+    D, rows = 64, []
+    near = [0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 0.5, 1.0, 3.0, 6.0, 6.9375, 0.0]
+    ulp = 2.0 ** -7 if io == "bf16" else 2.0 ** -23
+    for p in (-149, -130, -126, -125, -124, -60, 0, 1, 60, 124, 125):
+        body = [s * y * f for y in near for f in (1 - ulp, 1.0, 1 + ulp) for s in (1, -1)]
+        for top in (4.0, 6.0, 6.5, 7.0 - 4 * ulp, 7.0, 7.0 + 4 * ulp, 7.5):
+            small = [math.copysign(min(abs(b), top), b) for b in body]
+            vals = small[:31] + [top] + small[31:62] + [-top]
+            rows.append(torch.tensor(vals, dtype=torch.float64) * 2.0 ** p)
+            vals = small[-31:] + [-top] + small[40:71] + [top]
+            rows.append(torch.tensor(vals, dtype=torch.float64) * 2.0 ** p)
+    big = float(torch.finfo(DT[io]).max)
+    rows = torch.stack(rows).clamp(-big, big).to(DT[io])
+    odd = torch.ones((6, D), dtype=DT[io])
+    odd[0, 3], odd[1, 40], odd[2, 31], odd[3, :] = math.nan, math.inf, -math.inf, big
+    odd[4, 0], odd[5, 63] = -math.nan, torch.finfo(DT[io]).tiny
+    rows = torch.cat([rows, odd])[:, None]
+    n = rows.shape[0]
+    c = Cache4([n], H=1, G=1, D=D, page=16, io=io, seed=2)
+    slots = [int(c.table_h[0, t // 16]) * 16 + t % 16 for t in range(n)]
+    raw = append(c, rows, rows.flip(0), slots)
+    same_bytes(raw[0], *after(c, "k", rows, slots), 16, D)
+    same_bytes(raw[1], *after(c, "v", rows.flip(0), slots), 16, D)
+    k, v = gather(c.kv, [0] * n, list(range(n)), c.lengths, 1, D, io)
+    for got, want in ((k, stored4(rows)), (v, stored4(rows.flip(0)))):
+        assert torch.equal(torch.isnan(got), torch.isnan(want))
+        assert torch.equal(got.double().nan_to_num(9.0), want.nan_to_num(9.0))
+    # a block that is not finite leaves its neighbours alone
+    assert torch.isnan(k[-6, 0, :32]).all() and bool((k[-6, 0, 32:] == 1).all())
+    c.close()
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("D,page,n", [(64, 16, 5), (128, 64, 700), (256, 32, 130), (128, 16, 9000), (64, 256, 20000)])
+def test_bounds_hold_the_stored_keys(io, D, page, n):
+    """Also where a page's tokens are spread over several waves' runs."""
+    H = 1 if n > 1000 else 2
+    g = torch.Generator().manual_seed(n)
+    c = Cache4([n + 9], H=H, G=1, D=D, page=page, io=io, seed=3)
+    c.bounds_h = torch.randint(-5, 5, c.bounds_h.shape, generator=g).sort(dim=2).values.to(torch.int8)
+    c.bounds.copy_(c.bounds_h)
+    k, v = (torch.randn((n, H, D), generator=g).to(DT[io]) for _ in range(2))
+    if n < 1000:
+        k[2, 0, 5] = math.nan
+    slots = [int(c.table_h[0, t // page]) * page + t % page for t in range(9, n + 9)]
+    slots[-1] = -1
+    raw = append(c, k, v, slots)
+    same_bytes(raw[0], *after(c, "k", k, slots), page, D)
+    want = bounds_ref(c.bounds_h, stored4(k).float(), slots, torch.ones(H), c.step_h, "f32", page)
+    assert torch.equal(c.bounds.cpu(), torch.from_numpy(want))
+    c.close()
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("n", [1, 37, 9000])
+def test_gather_reads_rows_back(io, D, n):
+    """Any pairs in any order, the same one twice; pairs that name no row are left as they were."""
+    rng = random.Random(n)
+    lens = [0, 70, 1, 300]
+    c = Cache4(lens, H=3 if n < 1000 else 2, G=2, D=D, page=32, io=io, seed=4)
+    pairs = [(r, p) for r in (1, 2, 3) for p in range(lens[r])]
+    picked = [rng.choice(pairs) for _ in range(n)]
+    for i, bad in zip(range(1, n, 5), [(-1, -1), (0, 0), (1, 70), (3, -2), (4, 0), (2, 1 << 30), (-2 ** 31, 5)] * n):
+        picked[i] = bad
+    owners, positions = [r for r, _ in picked], [p for _, p in picked]
+    got = gather(c.kv, owners, positions, c.lengths, c.H, D, io, strides=(64, 8))
+    where = torch.tensor([0 <= r < 4 and 0 <= p < lens[r] for r, p in picked])
+    for x, rows in zip("kv", got):
+        assert bool((rows[~where] == 7.0).all())
+        r, p = torch.tensor(owners)[where], torch.tensor(positions)[where]
+        page, row = c.table_h[r.long(), p.long() // 32].long(), p.long() % 32
+        want = decode_ref(c.code[x][page, :, row], c.E[x][page, :, row])
+        assert torch.equal(rows[where].double(), want)
+    only_k = gather(c.kv, owners, positions, c.lengths, c.H, D, io, sides="k")
+    only_v = gather(c.kv, owners, positions, c.lengths, c.H, D, io, sides="v")
+    assert torch.equal(only_k[0], got[0]) and bool((only_k[1] == 7.0).all())
+    assert torch.equal(only_v[1], got[1]) and bool((only_v[0] == 7.0).all())
+    c.close()
+
+
+@pytest.mark.parametrize("io,cache", [("bf16", "bf16"), ("bf16", "fp8"), ("f32", "f32"), ("f32", "bf16"), ("f32", "fp8")])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_gather_reads_every_type(io, cache, D):
+    """Of 8 bits: the code times the scale, one product rounded to fp32, then to io."""
+    lens = [33, 0, 90]
+    c = Cache(lens, H=2, G=1, D=D, page=16, io=io, cache=cache, seed=D)
+    owners = [2] * 90 + [0] * 33 + [1, -1]
+    positions = list(range(89, -1, -1)) + list(range(33)) + [0, 0]
+    got = gather(c.kv, owners, positions, c.lengths, 2, D, io)
+    for x, rows, scale in zip("kv", got, (c.k_scale_h, c.v_scale_h)):
+        assert bool((rows[-2:] == 7.0).all())
+        for h in range(2):
+            for t in range(len(owners) - 2):
+                page, row = int(c.table_h[owners[t], positions[t] // 16]), positions[t] % 16
+                value = (c.k if x == "k" else c.v).float()[page, h, row]
+                assert torch.equal(rows[t, h], (value * scale[h] if cache == "fp8" else value).to(DT[io]))
+    c.close()
+
+
+# ---------------------------------------------------------------------------
+# attend
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("page", [16, 32, 64, 256])
+def test_attend_at_the_edges_of_tiles_and_pages(io, D, page):
+    c = Cache4(EDGES, H=2, G=3, D=D, page=page, io=io, seed=D + page)
+    got = c.attend()
+    for r in range(c.R):
+        c.check(got, r)
+    c.close()
+
+
+@pytest.mark.parametrize("H,G", [(1, 1), (3, 2), (1, 5), (2, 8), (1, 16), (2, 17), (1, 40), (1, 128)])
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_attend_head_layouts(H, G, io):
+    c = Cache4([70, 0, 33, 129], H=H, G=G, D=64, page=32, io=io, seed=G)
+    got = c.attend()
+    for r in range(c.R):
+        c.check(got, r)
+    c.close()
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_attend_long_rows_are_split_and_joined(io, D):
+    lens = [40000, 1, 0, 700, 5000, 31]
+    c = Cache4(lens, H=2, G=4, D=D, page=128, io=io, seed=5)
+    got = c.attend()
+    for r in range(c.R):
+        c.check(got, r)
+    again = c.attend()
+    assert torch.equal(got[0].float(), again[0].float()) and torch.equal(got[1], again[1])
+    c.close()
+
+
+def test_attend_many_short_rows_beside_long_ones():
+    rng = random.Random(3)
+    lens = [rng.choice([0, 1, 5, 16, 40, 90, 150]) for _ in range(700)]
+    lens[13], lens[400], lens[699] = 9000, 3000, 1
+    c = Cache4(lens, H=2, G=2, D=64, page=16, io="bf16", seed=6)
+    got = c.attend()
+    for r in list(range(0, 700, 9)) + [13, 400, 699]:
+        c.check(got, r)
+    c.close()
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("page", [16, 32, 256])
+@pytest.mark.parametrize("window", [1, 16, 31, 100, 1000])
+def test_attend_window(io, page, window):
+    c = Cache4([0, 1, 30, 100, 101, 999, 1001, 3001], H=2, G=2, D=128, page=page, io=io, seed=window)
+    got = c.attend(window=window)
+    for r in range(c.R):
+        c.check(got, r, window=window)
+    c.close()
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("page", [16, 32, 64])
+def test_attend_over_listed_pages(io, D, page):
+    lens = [0, 1, 40, 500, 1030, 2000]
+    c = Cache4(lens, H=2, G=4, D=D, page=page, io=io, seed=3)
+    rng, keep, lists = random.Random(4), 9, []
+    for r, n in enumerate(lens):
+        per = []
+        for h in range(c.H):
+            held = pages_of(n, page)
+            chosen = sorted(rng.sample(range(held), min(held, keep)))
+            if r == 3:
+                chosen[2] = -1
+            if r == 4:
+                chosen[-1] = held + 5
+            if r == 5 and h == 1:
+                chosen = [-1] * keep
+            per.append(chosen + [-1] * (keep - len(chosen)))
+        lists.append(per)
+    got = c.attend(pages=i32(lists))
+    for r in range(c.R):
+        c.check(got, r, listed=lists[r])
+    c.close()
+
+
+def test_attend_touches_the_listed_owners_only():
+    c = Cache4([40, 100, 0, 33, 257, 12], H=2, G=2, D=64, page=32, io="bf16", seed=8)
+    rows = [4, 2, -1, 0, 77]
+    out, lse = c.attend(rows=i32(rows))
+    for r in range(c.R):
+        if r in rows:
+            c.check((out, lse), r)
+        else:
+            assert bool((out[r] == 7.0).all()) and bool((lse[r] == 7.0).all())
+    c.close()
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_powers_far_apart(io):
+    """Blocks from 2^-100 to 2^110 in values, to 2^40 in keys: each enters with its own power.
+
+    Queries are zero in the blocks of large keys, so scores stay small; a value of
+    the largest power is alone in its channels."""
+    c = Cache4([3, 50], H=1, G=2, D=128, page=16, io=io, seed=9, poison=False)
+    c.E["k"][..., 0], c.E["k"][..., 1] = 127 - 100, 127 + 40
+    c.E["v"][..., 0], c.E["v"][..., 1] = 127 - 100, 127 + 110
+    c.E["v"][..., 2] += torch.randint(-40, 0, c.E["v"][..., 2].shape, generator=torch.Generator().manual_seed(1))
+    c.close()
+    c.upload()
+    c.q_h[..., 32:64] = 0.0
+    out, lse = c.attend()
+    for r in range(2):
+        ref, rl, _, ltol = c.attend_ref(r)
+        half = 2.0 ** -8 if io == "bf16" else 2.0 ** -24
+        for b in range(4):
+            d = slice(b * 32, b * 32 + 32)
+            most = float(c.rows_of(r, 0, "v", range(c.lens[r]))[:, d].abs().max())
+            # scores off by 132 2^-24 of their products' size (some tens), probabilities by twice that
+            delta = 132 * 2.0 ** -24 * 128 ** -0.5 * float(
+                (c.q_h[r].double().abs() @ c.rows_of(r, 0, "k", range(c.lens[r])).abs().t()).max())
+            err = (out[r][:, d].double() - ref[:, d]).abs()
+            assert bool((err <= half * 1.01 * ref[:, d].abs() + (2 * delta + 2.0 ** -16) * most).all()), (r, b)
+        assert bool(((lse[r].double() - rl).abs() <= ltol).all())
+    c.close()
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_a_row_that_is_not_finite_makes_its_head_nan(io):
+    """In the rows attended to, a NaN key makes the head NaN, a NaN value its block's channels."""
+    c = Cache4([50, 50], H=2, G=2, D=64, page=16, io=io, seed=10)
+    c.E["k"][int(c.table_h[0, 2]), 0, 3, 1] = 255
+    c.E["v"][int(c.table_h[1, 0]), 1, 7, 0] = 255
+    c.close()
+    c.upload()
+    out, lse = c.attend()
+    assert torch.isnan(out[0, :2]).all() and torch.isnan(lse[0, :2]).all()
+    assert torch.isnan(out[1, 2:, :32]).all()
+    assert torch.isfinite(out[0, 2:]).all() and torch.isfinite(out[1, :2]).all() and torch.isfinite(out[1, 2:, 32:]).all()
+    assert torch.isfinite(lse[1]).all()
+    out, _ = c.attend(window=2)                              # out of the window they have no influence
+    assert torch.isfinite(out).all()
+    c.close()
+
+
+def test_select_and_attend_after_append():
+    """A cache written by append alone: the selection by its bounds, then the attention over it."""
+    lens, H, G, D, page, keep = [300, 37, 129], 2, 3, 128, 16, 6
+    g = torch.Generator().manual_seed(11)
+    c = Cache4(lens, H=H, G=G, D=D, page=page, io="bf16", seed=11)
+    for r, n in enumerate(lens):
+        k, v = (torch.randn((n, H, D), generator=g).to(torch.bfloat16) for _ in range(2))
+        slots = [int(c.table_h[r, t // page]) * page + t % page for t in range(n)]
+        append(c, k, v, slots)
+        c.code["k"], c.E["k"] = after(c, "k", k, slots)
+        c.code["v"], c.E["v"] = after(c, "v", v, slots)
+    pages = torch.zeros((3, H, keep), dtype=torch.int32, device="cuda")
+    q = dev(c.q_h)
+    ok(KV.rwttt_kv_select(c.kv, 0, q.data_ptr(), q.stride(0), c.lengths.data_ptr(), 0, 3, 1, 2, keep, pages.data_ptr(), stream()))
+    got = c.attend(pages=pages)
+    bounds, lists = c.bounds.cpu().numpy(), pages.tolist()
+    for r, n in enumerate(lens):
+        held = c.table_h[r, :pages_of(n, page)].numpy()
+        for h in range(H):
+            want = select_ref(c.q_h[r, h * G:(h + 1) * G].float().numpy(), bounds[:, h], held, 1, 2, keep)
+            assert lists[r][h] == want
+        c.check(got, r, listed=lists[r])
+    c.close()
+
+
+def test_another_stream_and_a_graph():
+    """The same bits from another stream and from three replays of a captured store, read and attention,
+    with eager calls in between."""
+    c = Cache4([300, 37, 129], H=2, G=4, D=128, page=32, io="bf16", seed=12)
+    g = torch.Generator().manual_seed(1)
+    k, v = (dev(torch.randn((3, 2, 128), generator=g).to(torch.bfloat16)) for _ in range(2))
+    at = [299, 36, 128]
+    slots = i32([int(c.table_h[r, p // 32]) * 32 + p % 32 for r, p in enumerate(at)])
+    owners, positions, q = i32([0, 1, 2]), i32(at), dev(c.q_h)
+    ko, vo = (torch.zeros((3, 2, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    out = torch.zeros((3, 8, 128), dtype=torch.bfloat16, device="cuda")
+
+    def step():
+        ok(KV.rwttt_kv_append(c.kv, 0, k.data_ptr(), 256, v.data_ptr(), 256, slots.data_ptr(), 3, stream()))
+        ok(KV.rwttt_kv_gather(c.kv, 0, owners.data_ptr(), positions.data_ptr(), c.lengths.data_ptr(), 3, ko.data_ptr(), 256,
+                              vo.data_ptr(), 256, stream()))
+        ok(KV.rwttt_kv_attend(c.kv, 0, q.data_ptr(), 1024, c.lengths.data_ptr(), 0, 3, 0.1, 0, 0, 0, out.data_ptr(), 1024, 0,
+                              stream()))
+
+    step()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (ko, vo, out)]
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip((ko, vo, out), want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(3):
+        k.mul_(-1 if i else 1)
+        for t in (ko, vo, out):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (ko, vo, out)]
+        step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((ko, vo, out), got))
+        if i == 0:
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+    c.close()
