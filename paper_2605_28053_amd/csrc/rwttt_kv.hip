@@ -830,8 +830,23 @@ constexpr int kAttWaves = kAttThreads / 64;
 constexpr int kJoinWindow = 32, kJoinDirect = 48;
 constexpr int kAttPad = 4;               // floats behind a query's sums in LDS: neighbours in other banks
 
-// Rows of keys a wave takes at a time.
-constexpr int tile_rows(int ct) { return ct == RWTTT_F32 ? 16 : 32; }
+// Rows of keys a wave takes at a time.  Of 4 bits (540 MB at 128 channels, 280 at 64):
+// 97 us with 32 rows and three blocks a CU, 99 with 64 and two, 105 with 32 and two;
+// 62.6 us with 64 rows and three blocks, 66 with 32 and three or four; at 256 channels
+// 59.5 us with 32 rows, 62.5 with 64.
+constexpr int tile_rows(int ct, int dim) {
+  return ct == RWTTT_FP4 ? (dim == 64 ? 64 : 32) : ct == RWTTT_F32 ? 16 : 32;
+}
+
+// Blocks of a call that a CU holds, and the chip.  What the registers leave room for:
+// at 256 channels no more than one (16 owners of 8500 rows: 180 us in bf16 and 94 in
+// e4m3 so, 184 and 102 with twice the blocks; two of 4 bits take 57.7 us instead of
+// 59.5, but 20.8 instead of 19.0 over selected pages).
+constexpr int blocks_a_cu(int io, int ct, int dim) {
+  if (dim == 256) return 1;
+  return ct == RWTTT_FP4 && (io || dim == 64) ? 3 : 2;
+}
+constexpr int blocks_of(int io, int ct, int dim) { return 256 * blocks_a_cu(io, ct, dim); }
 
 struct RowRange {
   int base, tiles, held;                 // base: first tile's first row; held: listed pages
@@ -942,27 +957,13 @@ template <int N> __device__ __forceinline__ void split_bf16(const float* x, bf16
 //           each of the KT / 4 rows of the lane's group
 template <int CT, int D> struct TileShape {
   static constexpr int B = CT == RWTTT_F32 ? 4 : CT == RWTTT_BF16 ? 2 : 1;
-  static constexpr int KT = tile_rows(CT), NT = KT / 16;
+  static constexpr int KT = tile_rows(CT, D), NT = KT / 16;
   static constexpr int KE = 16 / B, KW = D / (4 * KE);
   static constexpr int VE = D / 16 < KE ? D / 16 : KE, NE = D / 16 / VE, VW = VE * B / 4;
   static constexpr int VR = KT / 4;      // rows of values a lane holds
   static constexpr int NA = D / 16;      // output tiles (four channels a lane)
-  static constexpr int PER = CT == RWTTT_F32 ? 1 : KE / 8;   // operands that a piece of keys feeds
   __device__ static int key_channel(int s, int g) { return (s * 4 + g) * KE; }
   __device__ static int value_channel(int e, int c) { return (e * 16 + c) * VE; }
-};
-
-// Of 4 bits: pieces of 32 channels (16 where a row has no more than 64), a block's or
-// half of one's, and in one lane the D / 16 values of one of a block's channels.
-template <int D> struct TileShape<RWTTT_FP4, D> {
-  static constexpr int KT = tile_rows(RWTTT_FP4), NT = KT / 16;
-  static constexpr int KE = D == 64 ? 16 : 32, KW = D / (4 * KE);
-  static constexpr int VE = D / 16, NE = 1, VW = VE <= 8 ? 1 : VE / 8;
-  static constexpr int VR = KT / 4;
-  static constexpr int NA = D / 16;
-  static constexpr int PER = KE / 8;
-  __device__ static int key_channel(int s, int g) { return (s * 4 + g) * KE; }
-  __device__ static int value_channel(int, int c) { return c * VE; }
 };
 
 // Which pages a tile's halves (16 rows each) lie in, and which of their rows count.
@@ -971,9 +972,15 @@ template <int NT> struct TileAt {
   int off[NT], from[NT], to[NT];         // rows [from, to) of the half count
 };
 
-template <int IO, int CT, int D, bool NT_HINT>
-__global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kernel(const AttendParams ap) {
-  using S = TileShape<CT, D>;
+#include "rwttt_kv_attend4.h"
+
+template <int CT, int D> struct AttendTile { using type = TileShape<CT, D>; };
+template <int D> struct AttendTile<RWTTT_FP4, D> { using type = TileShape4<D>; };
+
+// TG: of a 4-bit cache, the terms of a probability that one product takes (1 to 3); 1 otherwise.
+template <int IO, int CT, int D, bool NT_HINT, int TG>
+__global__ void __launch_bounds__(kAttThreads, blocks_a_cu(IO, CT, D)) kv_attend_kernel(const AttendParams ap) {
+  using S = typename AttendTile<CT, D>::type;
   constexpr int KT = S::KT, NT = S::NT;
   constexpr bool F = CT == RWTTT_F32, X = CT == RWTTT_FP4;
   constexpr int NQ = IO ? 1 : 3, NP = 3;               // bf16 terms of a query, of a probability
@@ -1052,6 +1059,17 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
     const scalar_i32 table = scalar(p.table + size_t(owner) * p.s.max_pages);
     const scalar_i32 list = scalar(p.pages ? p.pages + (size_t(owner) * H + h) * p.keep : nullptr);
 
+    float m = -INFINITY, l = 0.f;
+    f32x4_t acc[S::NA];
+#pragma unroll
+    for (int a = 0; a < S::NA; ++a) acc[a] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+
+    if constexpr (X) {
+      const int32_t* listed = p.pages ? p.pages + (size_t(owner) * H + h) * p.keep : nullptr;
+      const Rows4 at4{p.table + size_t(owner) * p.s.max_pages, listed, p.k, p.v, h, base, held, len, least,
+                      last_page, t0, t1};
+      attend_rows4<IO, D, NT_HINT, TG>(p, at4, ap.scale_log2, owner, head0, heads, m, l, acc);
+    } else {
     auto locate = [&](int t) {
       TileAt<NT> at;
 #pragma unroll
@@ -1074,7 +1092,7 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
     };
 
     // queries: the lane's column is one of them; piece s of its channels feeds PER operands
-    constexpr int PER = S::PER, QN = F ? D / 16 : D / 32, QW = F || IO ? 4 : 8;
+    constexpr int PER = F ? 1 : S::KE / 8, QN = F ? D / 16 : D / 32, QW = F || IO ? 4 : 8;
     const char* q_at = static_cast<const char*>(p.q) +
                        (size_t(owner) * p.q_stride + (size_t(h) * G + head0 + (c < heads ? c : 0)) * D) * (IO ? 2 : 4);
     uint32_t qw[QN][QW];
@@ -1086,27 +1104,14 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
     }
     const float to_log2 = ap.scale_log2 * (CT == RWTTT_FP8 && p.k_scale ? p.k_scale[h] : 1.f);
 
-    float m = -INFINITY, l = 0.f;
-    f32x4_t acc[S::NA];
-#pragma unroll
-    for (int a = 0; a < S::NA; ++a) acc[a] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-
     uint32_t kw[NT][S::KW][4];
     uint32_t vw[S::NE][S::VR][S::VW];
-    uint32_t kp[X ? NT : 1][X ? S::KW : 1], vp[2];   // 4 bits: powers of the pieces, of the lane's rows
     // row of a half that the lane loads: keys, one a lane; values, VR in turn
     const int k_half = NT == 2 ? c >> 3 : 0, v_half = NT == 2 ? g >> 1 : 0;
     auto half_of = [&](const TileAt<NT>& at, const void* cache, int half) {
       const uint32_t page = NT == 2 && half ? at.page[NT - 1] : at.page[0];
       const int off = NT == 2 && half ? at.off[NT - 1] : at.off[0];
-      const size_t chunk = size_t(page) * H + h;
-      if constexpr (X) return static_cast<const char*>(cache) + chunk * fp4_chunk(P, D) + off * (D / 2);
-      else return static_cast<const char*>(cache) + (chunk * P + off) * size_t(D * S::B);
-    };
-    // From a half's first row of 4 bits to the power of its block b.
-    auto power_of = [&](const TileAt<NT>& at, int half, int b) {
-      const int off = NT == 2 && half ? at.off[NT - 1] : at.off[0];
-      return fp4_power(P, D, b, off) - off * (D / 2);
+      return static_cast<const char*>(cache) + ((size_t(page) * H + h) * P + off) * size_t(D * S::B);
     };
     auto load_keys = [&](const TileAt<NT>& at) {
       const char* src = half_of(at, p.k, k_half);
@@ -1114,29 +1119,11 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
       for (int t = 0; t < NT; ++t) {
         const int rr = NT == 2 ? ((c >> 2) & 1) * 8 + t * 4 + (c & 3) : c;
 #pragma unroll
-        for (int s = 0; s < S::KW; ++s) {
-          if constexpr (X) {
-            load_words<S::KE / 8, NT_HINT>(src + (rr * D + S::key_channel(s, g)) / 2, kw[t][s]);
-            kp[t][s] = *reinterpret_cast<const uint8_t*>(
-                src + power_of(at, k_half, S::key_channel(s, g) / RWTTT_KV_BLOCK) + rr);
-          } else {
-            load_words<4, NT_HINT>(src + (rr * D + S::key_channel(s, g)) * S::B, kw[t][s]);
-          }
-        }
+        for (int s = 0; s < S::KW; ++s) load_words<4, NT_HINT>(src + (rr * D + S::key_channel(s, g)) * S::B, kw[t][s]);
       }
     };
     auto load_values = [&](const TileAt<NT>& at) {
       const char* src = half_of(at, p.v, v_half);
-      if constexpr (X) {
-#pragma unroll
-        for (int k = 0; k < S::VR; ++k) {
-          const char* row = src + (((g & 1) * 8 + k) * D + S::value_channel(0, c)) / 2;
-          if constexpr (D == 64) vw[0][k][0] = *reinterpret_cast<const uint16_t*>(row);
-          else load_words<S::VW, NT_HINT>(row, vw[0][k]);
-        }
-        load_words<2>(src + power_of(at, v_half, S::value_channel(0, c) / RWTTT_KV_BLOCK) + (g & 1) * 8, vp);
-        return;
-      } else {
 #pragma unroll
       for (int e = 0; e < S::NE; ++e)
 #pragma unroll
@@ -1144,7 +1131,6 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
           const int rr = NT == 2 ? (g & 1) * 8 + k : g * 4 + k;
           load_words<S::VW, NT_HINT>(src + (rr * D + S::value_channel(e, c)) * S::B, vw[e][k]);
         }
-      }
     };
 
     TileAt<NT> at = locate(min(t0, seg1 - 1)), next = at;
@@ -1198,10 +1184,6 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
             bf16x8_t key;
             if constexpr (CT == RWTTT_BF16) {
               key = as_bf16x8(kw[k][a]);
-            } else if constexpr (X) {
-              uint32_t wd[4];
-              fp4_octet(kw[k][a / PER][a % PER], fp4_unit(kp[k][a / PER]), wd);
-              key = as_bf16x8(wd);
             } else {
               uint32_t wd[4];
 #pragma unroll
@@ -1254,11 +1236,6 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
           for (int j = 0; j < S::VR; ++j)
 #pragma unroll
             for (int b = 0; b < S::VW; ++b) vw[e][j][b] = j >= from && j < to ? vw[e][j][b] : 0u;
-        if constexpr (X) {               // a power of such a row may be the NaN's
-#pragma unroll
-          for (int j = 0; j < S::VR; ++j)
-            if (j < from || j >= to) vp[j / 4] = (vp[j / 4] & ~(0xffu << (8 * (j % 4)))) | 127u << (8 * (j % 4));
-        }
       }
       if constexpr (F) {
 #pragma unroll
@@ -1272,27 +1249,6 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
       } else {
         bf16x8_t pt[NP];
         split_bf16<NP>(pr, pt);
-        if constexpr (X) {
-          // two rows' pairs of channels, then two channels' pairs of rows
-#pragma unroll
-          for (int a = 0; a < S::VE; a += 2) {
-            uint32_t even[4], odd[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float u0 = fp4_unit(vp[j / 2] >> (16 * (j % 2)) & 0xffu), u1 = fp4_unit(vp[j / 2] >> (16 * (j % 2) + 8) & 0xffu);
-              const uint32_t x = fp4_pair_at(vw[0][2 * j][a / 8], u0, a / 2 % 4);
-              const uint32_t y = fp4_pair_at(vw[0][2 * j + 1][a / 8], u1, a / 2 % 4);
-              even[j] = __builtin_amdgcn_perm(y, x, 0x05040100u);
-              odd[j] = __builtin_amdgcn_perm(y, x, 0x07060302u);
-            }
-            const bf16x8_t v0 = as_bf16x8(even), v1 = as_bf16x8(odd);
-#pragma unroll
-            for (int b = NP - 1; b >= 0; --b) {
-              acc[a] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pt[b], acc[a], 0, 0, 0);
-              acc[a + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pt[b], acc[a + 1], 0, 0, 0);
-            }
-          }
-        } else {
 #pragma unroll
         for (int e = 0; e < S::NE; ++e)
 #pragma unroll
@@ -1315,31 +1271,34 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
               acc[e * S::VE + a] =
                   __builtin_amdgcn_mfma_f32_16x16x32_bf16(val, pt[b], acc[e * S::VE + a], 0, 0, 0);
           }
-        }
       }
       if (more) {
         load_values(next);
         at = next;
       }
     }
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
+    }
+    if constexpr (!X) {
+      l += __shfl_xor(l, 16);
+      l += __shfl_xor(l, 32);
+    }
 
     // the waves' sums into LDS: acc[e * VE + a][j] is channel
-    // value_channel(e, 4 g + j) + a of query c
+    // value_channel(e, 4 g + j) + a of query c (of TG terms apart: of query c % heads)
     constexpr int DP = D + kAttPad;
+    const int columns = heads * TG;
     if (g == 0) {
       wave_ml[wave][c][0] = m;
       wave_ml[wave][c][1] = l;
     }
-    if (c < heads) {
+    if (c < columns) {
 #pragma unroll
       for (int e = 0; e < S::NE; ++e)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
           for (int a = 0; a < S::VE; a += 4)
-            *reinterpret_cast<f32x4_t*>(wave_acc + (wave * heads + c) * DP + S::value_channel(e, g * 4 + j) + a) =
+            *reinterpret_cast<f32x4_t*>(wave_acc + (wave * columns + c) * DP + S::value_channel(e, g * 4 + j) + a) =
                 (f32x4_t){acc[e * S::VE + a][j], acc[e * S::VE + a + 1][j], acc[e * S::VE + a + 2][j],
                           acc[e * S::VE + a + 3][j]};
     }
@@ -1375,8 +1334,15 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
 #pragma unroll
       for (int v = 0; v < kAttWaves; ++v) {
         const float mv = wave_ml[v][head][0], f = mv == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mv - top);
-        sum += f * *reinterpret_cast<const f32x4_t*>(wave_acc + (v * heads + head) * DP + col * 4);
-        sl += f * wave_ml[v][head][1];
+        f32x4_t x = *reinterpret_cast<const f32x4_t*>(wave_acc + (v * columns + head) * DP + col * 4);
+#pragma unroll
+        for (int t = 1; t < TG; ++t)
+          x += *reinterpret_cast<const f32x4_t*>(wave_acc + (v * columns + t * heads + head) * DP + col * 4);
+        sum += f * x;
+        float xl = wave_ml[v][head][1];
+#pragma unroll
+        for (int t = 1; t < TG; ++t) xl += wave_ml[v][t * heads + head][1];
+        sl += f * xl;
       }
       if (complete) {
         write_out(head, col, sum, top, sl);
@@ -1472,7 +1438,11 @@ __global__ void __launch_bounds__(kAttThreads, D == 256 ? 1 : 2) kv_attend_kerne
   }
 }
 
-constexpr int kAttBlocks = 512;          // two a CU
+// Blocks that a workspace has room for.
+int most_blocks(const KvShape& s) {
+  const int blocks = blocks_of(s.io_bf16, s.cache, s.head_dim);
+  return blocks < 512 ? 512 : blocks;
+}
 
 int part_heads_of(int group) { return group < 16 ? group : 16; }
 
@@ -1495,10 +1465,10 @@ struct KvWorkspace {
       used += (n + 255) / 256 * 256;
       return q;
     };
-    const size_t windows = kAttBlocks / kJoinWindow * 2;
-    const size_t slots = (size_t(kAttBlocks) * 2 + windows) * part_heads_of(s.group);
+    const size_t blocks = most_blocks(s), windows = blocks / kJoinWindow * 2;
+    const size_t slots = (blocks * 2 + windows) * part_heads_of(s.group);
     const size_t rows = select_rows(s);
-    attend_count = reinterpret_cast<uint32_t*>(take((kAttBlocks + windows) * sizeof(uint32_t)));
+    attend_count = reinterpret_cast<uint32_t*>(take((blocks + windows) * sizeof(uint32_t)));
     select_count = reinterpret_cast<uint32_t*>(take(kSelRows * sizeof(uint32_t)));
     part = reinterpret_cast<float*>(take(slots * s.head_dim * sizeof(float)));
     part_ml = reinterpret_cast<float*>(take(slots * 2 * sizeof(float)));
@@ -1550,13 +1520,13 @@ template <int IO, int CT> hipError_t append_dims(const AppendParams& p, hipStrea
                                  : append_go<IO, CT, 256>(p, stream);
 }
 
-template <int IO, int CT, int D> hipError_t attend_go(AttendParams p, hipStream_t stream) {
+template <int IO, int CT, int D, int TG> hipError_t attend_terms(AttendParams p, hipStream_t stream) {
   const uint64_t rows = uint64_t(p.L.n) * p.L.s.kv_heads * p.head_tiles;
-  const dim3 grid(unsigned(attend_grid(rows, p.L.s.max_pages << p.L.s.page_shift, tile_rows(CT), p.blocks)));
-  const int acc = kAttWaves * p.part_heads * (D + kAttPad), join = kAttThreads * 6;
+  const dim3 grid(unsigned(attend_grid(rows, p.L.s.max_pages << p.L.s.page_shift, tile_rows(CT, D), p.blocks)));
+  const int acc = kAttWaves * p.part_heads * TG * (D + kAttPad), join = kAttThreads * 6;
   p.acc_words = acc < join ? join : acc;
   const size_t lds = (p.acc_words + row_table_words(int(p.L.n))) * sizeof(float);
-  auto kernel = p.stream ? kv_attend_kernel<IO, CT, D, true> : kv_attend_kernel<IO, CT, D, false>;
+  auto kernel = p.stream ? kv_attend_kernel<IO, CT, D, true, TG> : kv_attend_kernel<IO, CT, D, false, TG>;
   if (lds > 60 * 1024) {                 // more than 64 KB of the CU's 160 KB has to be asked for
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                              hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
@@ -1564,6 +1534,17 @@ template <int IO, int CT, int D> hipError_t attend_go(AttendParams p, hipStream_
   }
   hipLaunchKernelGGL(kernel, grid, dim3(kAttThreads), lds, stream, p);
   return hipGetLastError();
+}
+
+template <int IO, int CT, int D> hipError_t attend_go(const AttendParams& p, hipStream_t stream) {
+  if constexpr (CT == RWTTT_FP4) {
+    const int terms = terms4(p.L.s.group);
+    return terms == 3   ? attend_terms<IO, CT, D, 3>(p, stream)
+           : terms == 2 ? attend_terms<IO, CT, D, 2>(p, stream)
+                        : attend_terms<IO, CT, D, 1>(p, stream);
+  } else {
+    return attend_terms<IO, CT, D, 1>(p, stream);
+  }
 }
 
 template <int IO, int CT> hipError_t attend_dims(const AttendParams& p, hipStream_t stream) {
@@ -1621,10 +1602,7 @@ hipError_t launch_kv_select(const KvSelectLaunch& L, hipStream_t stream) {
 hipError_t launch_kv_attend(const KvAttendLaunch& L, hipStream_t stream) {
   AttendParams p;
   p.L = L;
-  // What is resident at once: two blocks a CU, one for 256 channels, whose registers
-  // leave room for no more (16 owners of 8500 rows: 180 us in bf16 and 94 in e4m3 so,
-  // 184 and 102 with twice the blocks).
-  p.blocks = L.s.head_dim == 256 ? kAttBlocks / 2 : kAttBlocks;
+  p.blocks = blocks_of(L.s.io_bf16, L.s.cache, L.s.head_dim);
   p.head_tiles = (L.s.group + 15) / 16;
   p.part_heads = part_heads_of(L.s.group);
   const KvWorkspace ws(L.workspace, L.s);

@@ -25,6 +25,12 @@ __device__ __forceinline__ constexpr size_t fp4_power(int page_rows, int dim, in
 // 2^(e - 127) for a byte e: exponent 255 makes the conversions below NaN.
 __device__ __forceinline__ float fp4_unit(uint32_t e) { return __uint_as_float(e << 23); }
 
+// The unit of byte i of four.  Their neighbours' bits stay in the sign and the
+// mantissa, which the conversions do not read.
+__device__ __forceinline__ float fp4_unit_of(uint32_t four, int i) {
+  return __uint_as_float(i < 3 ? four << (23 - 8 * i) : four >> 1);
+}
+
 // Codes 2 b and 2 b + 1 of a word as bf16, times the unit: exact.
 template <int B> __device__ __forceinline__ uint32_t fp4_pair(uint32_t w, float unit) {
   const bf16x2_t h = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, unit, B);
