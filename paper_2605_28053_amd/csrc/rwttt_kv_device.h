@@ -93,7 +93,7 @@ template <int IO, int CT, int D> struct CachedRow {
     }
   }
   // Rounded once to the io type; scale is an 8-bit cache's.
-  __device__ __forceinline__ void store(char* dst, float scale) const {
+  template <bool HINT> __device__ __forceinline__ void store(char* dst, float scale) const {
     uint32_t o[4];
     if constexpr (CT == RWTTT_FP4) {
       const float unit = fp4_unit(power);
@@ -121,6 +121,8 @@ template <int IO, int CT, int D> struct CachedRow {
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[i] = w[i];
     }
-    *reinterpret_cast<u32x4_t*>(dst) = (u32x4_t){o[0], o[1], o[2], o[3]};
+    const u32x4_t t = {o[0], o[1], o[2], o[3]};
+    if (HINT) __builtin_nontemporal_store(t, reinterpret_cast<u32x4_t*>(dst));
+    else *reinterpret_cast<u32x4_t*>(dst) = t;
   }
 };

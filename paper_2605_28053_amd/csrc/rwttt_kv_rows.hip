@@ -25,6 +25,9 @@ namespace {
 // pairs, so a row may be turned in place: with HALF 16 bytes of each partner, with
 // INTERLEAVED 16 bytes.  Where a half of the turning channels is no whole number
 // of 16 bytes, a lane owns one pair.
+//
+// Bound by the bytes for a prefill: 8192 tokens of 32 + 8 heads of 128 channels in bf16
+// (168 MB in and out) take 27 us, 6.1 TB/s; a decode step of eight tokens 3.2 us.
 
 constexpr int kRotThreads = 256;
 
@@ -36,8 +39,10 @@ template <int IO> struct IoRow {           // 16 bytes of io
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = t[i];
   }
-  __device__ __forceinline__ void store(char* p) const {
-    *reinterpret_cast<u32x4_t*>(p) = (u32x4_t){w[0], w[1], w[2], w[3]};
+  template <bool HINT> __device__ __forceinline__ void store(char* p) const {
+    const u32x4_t t = {w[0], w[1], w[2], w[3]};
+    if (HINT) __builtin_nontemporal_store(t, reinterpret_cast<u32x4_t*>(p));
+    else *reinterpret_cast<u32x4_t*>(p) = t;
   }
   __device__ __forceinline__ float get(int i) const {
     if constexpr (IO) return i & 1 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]);
@@ -66,14 +71,16 @@ __device__ __forceinline__ float2 turned(float2 x, float2 cs) {
   return make_float2(fmaf(x.x, cs.x, -(x.y * cs.y)), fmaf(x.y, cs.x, x.x * cs.y));
 }
 
-template <int IO, Turn T>
+template <int IO, Turn T, int U>
 __global__ void __launch_bounds__(kRotThreads) kv_rotate_kernel(const RotateParams rp) {
   const KvRotateLaunch& p = rp.L;
   constexpr int B = IO ? 2 : 4, E = IoRow<IO>::E;
+  constexpr bool HINT = U > 1;
+  using M = Elem<std::conditional_t<IO, uint16_t, float>>;
   extern __shared__ float2 cs[];         // [tokens][turning / 2]: gain cos, gain sin
   const int half = p.turning / 2, n = int(p.n);
   const int t0 = blockIdx.x * rp.tokens, nt = min(rp.tokens, n - t0);
-  const int u0 = blockIdx.y * rp.part, u1 = min(rp.per_token, u0 + rp.part);
+  const int u0 = blockIdx.y * rp.part, span = min(rp.per_token, u0 + rp.part) - u0, total = nt * span;
 
   for (int i = threadIdx.x; i < nt * half; i += kRotThreads) {
     const int pos = p.positions[t0 + i / half];
@@ -82,62 +89,82 @@ __global__ void __launch_bounds__(kRotThreads) kv_rotate_kernel(const RotatePara
     sincospif(float(place) * 0x1p-63f, &s, &c);
     cs[i] = make_float2(c * p.gain, (p.inverse ? -s : s) * p.gain);
   }
-  __syncthreads();
-
-  const int span = u1 - u0;
-  for (int i = threadIdx.x; i < nt * span; i += kRotThreads) {
-    const int t = i / span, u = u0 + i % span;
-    if (p.positions[t0 + t] < 0) continue;
-    int h = u / rp.units;
-    const int x = u % rp.units;
-    const bool is_k = h >= p.q.heads;
-    const KvTurnRows& rows = is_k ? p.k : p.q;
-    h -= is_k ? p.q.heads : 0;
-    const char* src = static_cast<const char*>(rows.in) + ((t0 + t) * rows.in_stride + size_t(h) * p.head_dim) * B;
-    char* dst = static_cast<char*>(rows.out) + ((t0 + t) * rows.out_stride + size_t(h) * p.head_dim) * B;
-    const float2* at = cs + t * half;
-    if constexpr (T == Turn::half) {
-      const int pairs = half / E;
-      if (x < pairs) {
-        IoRow<IO> a, b;
-        a.load(src + x * 16);
-        b.load(src + half * B + x * 16);
-        IoRow<IO> ra, rb;
+  bool waited = false;
+  for (int i0 = threadIdx.x; i0 < total || !waited; i0 += U * kRotThreads) {
+    // U units, their loads in flight together
+    struct Unit {
+      char* dst;
+      const float2* at;
+      int x;                             // -1: none
+      IoRow<IO> a, b;
+      float2 pair;
+    } un[U];
 #pragma unroll
-        for (int j = 0; j < E; j += 2) {
-          const float2 y0 = turned(make_float2(a.get(j), b.get(j)), at[x * E + j]);
-          const float2 y1 = turned(make_float2(a.get(j + 1), b.get(j + 1)), at[x * E + j + 1]);
-          ra.put_pair(j / 2, y0.x, y1.x);
-          rb.put_pair(j / 2, y0.y, y1.y);
-        }
-        ra.store(dst + x * 16);
-        rb.store(dst + half * B + x * 16);
+    for (int j = 0; j < U; ++j) {
+      Unit& w = un[j];
+      const int i = i0 + j * kRotThreads;
+      w.x = -1;
+      if (i >= total) continue;
+      const int t = i / span, u = u0 + i % span;
+      if (p.positions[t0 + t] < 0) continue;
+      int h = u / rp.units;
+      w.x = u % rp.units;
+      const bool is_k = h >= p.q.heads;
+      const KvTurnRows& rows = is_k ? p.k : p.q;
+      h -= is_k ? p.q.heads : 0;
+      const char* src = static_cast<const char*>(rows.in) + ((t0 + t) * rows.in_stride + size_t(h) * p.head_dim) * B;
+      w.dst = static_cast<char*>(rows.out) + ((t0 + t) * rows.out_stride + size_t(h) * p.head_dim) * B;
+      w.at = cs + t * half;
+      if constexpr (T == Turn::half) {
+        const int pairs = half / E;
+        w.a.load(src + (w.x < pairs ? w.x : w.x + pairs) * 16);
+        if (w.x < pairs) w.b.load(src + half * B + w.x * 16);
+      } else if constexpr (T == Turn::interleaved) {
+        w.a.load(src + w.x * 16);
       } else {
-        IoRow<IO> a;
-        a.load(src + (x + pairs) * 16);
-        a.store(dst + (x + pairs) * 16);
+        w.pair = make_float2(w.x < half ? M::get(src, w.x) : 0.f, M::get(src, w.x + half));
       }
-    } else if constexpr (T == Turn::interleaved) {
-      IoRow<IO> a, r;
-      a.load(src + x * 16);
-      r = a;
+    }
+    if (!waited) __syncthreads();
+    waited = true;
 #pragma unroll
-      for (int j = 0; j < E / 2; ++j) {
-        const int k = x * (E / 2) + j;
-        if (k < half) {
-          const float2 y = turned(make_float2(a.get(2 * j), a.get(2 * j + 1)), at[k]);
-          r.put_pair(j, y.x, y.y);
+    for (int j = 0; j < U; ++j) {
+      Unit& w = un[j];
+      if (w.x < 0) continue;
+      if constexpr (T == Turn::half) {
+        const int pairs = half / E;
+        if (w.x < pairs) {
+          IoRow<IO> ra, rb;
+#pragma unroll
+          for (int e = 0; e < E; e += 2) {
+            const float2 y0 = turned(make_float2(w.a.get(e), w.b.get(e)), w.at[w.x * E + e]);
+            const float2 y1 = turned(make_float2(w.a.get(e + 1), w.b.get(e + 1)), w.at[w.x * E + e + 1]);
+            ra.put_pair(e / 2, y0.x, y1.x);
+            rb.put_pair(e / 2, y0.y, y1.y);
+          }
+          ra.template store<HINT>(w.dst + w.x * 16);
+          rb.template store<HINT>(w.dst + half * B + w.x * 16);
+        } else {
+          w.a.template store<HINT>(w.dst + (w.x + pairs) * 16);
         }
-      }
-      r.store(dst + x * 16);
-    } else {
-      using M = Elem<std::conditional_t<IO, uint16_t, float>>;
-      if (x < half) {
-        const float2 y = turned(make_float2(M::get(src, x), M::get(src, x + half)), at[x]);
-        M::put(dst, x, y.x);
-        M::put(dst, x + half, y.y);
+      } else if constexpr (T == Turn::interleaved) {
+#pragma unroll
+        for (int e = 0; e < E / 2; ++e) {
+          const int k = w.x * (E / 2) + e;
+          if (k < half) {
+            const float2 y = turned(make_float2(w.a.get(2 * e), w.a.get(2 * e + 1)), w.at[k]);
+            w.a.put_pair(e, y.x, y.y);
+          }
+        }
+        w.a.template store<HINT>(w.dst + w.x * 16);
       } else {
-        M::put(dst, x + half, M::get(src, x + half));
+        if (w.x < half) {
+          const float2 y = turned(w.pair, w.at[w.x]);
+          M::put(w.dst, w.x, y.x);
+          M::put(w.dst, w.x + half, y.y);
+        } else {
+          M::put(w.dst, w.x + half, w.pair.y);
+        }
       }
     }
   }
@@ -149,7 +176,9 @@ __global__ void __launch_bounds__(kRotThreads) kv_rotate_kernel(const RotatePara
 //
 // A wave takes one kv head of a run of rows: LPR lanes hold a row, 16 bytes of
 // output each, and the loads of its keys and values are in flight at once behind
-// the chain owner -> length and page.
+// the chain owner -> length and page.  Bound by the bytes, of which the output is the
+// most: 48700 rows of eight heads of 128 channels from 4 bits to bf16 (253 MB) take
+// 42 us, 6.0 TB/s, with non-temporal stores, 75 without; 500 rows 3.4 us.
 
 struct GatherParams {
   KvGatherLaunch L;
@@ -193,8 +222,8 @@ __global__ void __launch_bounds__(256) kv_gather_kernel(const GatherParams gp) {
     const size_t t = size_t(t0 + j * RPI + sub);
     if (page[j] >= 0) {
       const size_t col = size_t(h) * D * IOB + piece * 16;
-      if (p.k_out) k[j].store(static_cast<char*>(p.k_out) + t * p.k_stride * IOB + col, ks);
-      if (p.v_out) v[j].store(static_cast<char*>(p.v_out) + t * p.v_stride * IOB + col, vs);
+      if (p.k_out) k[j].template store<true>(static_cast<char*>(p.k_out) + t * p.k_stride * IOB + col, ks);
+      if (p.v_out) v[j].template store<true>(static_cast<char*>(p.v_out) + t * p.v_stride * IOB + col, vs);
     }
   }
 }
@@ -202,11 +231,13 @@ __global__ void __launch_bounds__(256) kv_gather_kernel(const GatherParams gp) {
 template <int IO, int CT, int D> hipError_t gather_go(GatherParams p, hipStream_t stream) {
   constexpr int RPI = 64 * (IO ? 8 : 4) / D;
   const uint64_t rows = uint64_t(p.L.n) * p.L.s.kv_heads;
-  const bool many = rows >= 4096u * 4 * RPI;
-  p.run = many ? 4 * RPI : RPI;
+  // two loads of rows a wave where that still makes eight waves a SIMD (256 MB of 128
+  // channels in bf16 42.4 us, in fp32 104; with one 43.3 and 107, with four 43.4 and 104)
+  const bool many = rows >= 8192u * 2 * RPI;
+  p.run = many ? 2 * RPI : RPI;
   const uint64_t units = uint64_t((p.L.n + p.run - 1) / p.run) * p.L.s.kv_heads;
   const dim3 grid(unsigned((units + 3) / 4)), block(256);
-  if (many) hipLaunchKernelGGL((kv_gather_kernel<IO, CT, D, 4>), grid, block, 0, stream, p);
+  if (many) hipLaunchKernelGGL((kv_gather_kernel<IO, CT, D, 2>), grid, block, 0, stream, p);
   else hipLaunchKernelGGL((kv_gather_kernel<IO, CT, D, 1>), grid, block, 0, stream, p);
   return hipGetLastError();
 }
@@ -217,10 +248,10 @@ template <int IO, int CT> hipError_t gather_dims(const GatherParams& p, hipStrea
                                  : gather_go<IO, CT, 256>(p, stream);
 }
 
-template <int IO> hipError_t rotate_go(const RotateParams& p, Turn how, dim3 grid, size_t lds, hipStream_t stream) {
-  auto kernel = how == Turn::half          ? kv_rotate_kernel<IO, Turn::half>
-                : how == Turn::interleaved ? kv_rotate_kernel<IO, Turn::interleaved>
-                                           : kv_rotate_kernel<IO, Turn::pairs>;
+template <int IO, int U> hipError_t rotate_go(const RotateParams& p, Turn how, dim3 grid, size_t lds, hipStream_t stream) {
+  auto kernel = how == Turn::half          ? kv_rotate_kernel<IO, Turn::half, U>
+                : how == Turn::interleaved ? kv_rotate_kernel<IO, Turn::interleaved, U>
+                                           : kv_rotate_kernel<IO, Turn::pairs, U>;
   hipLaunchKernelGGL(kernel, grid, dim3(kRotThreads), lds, stream, p);
   return hipGetLastError();
 }
@@ -250,12 +281,19 @@ hipError_t launch_kv_rotate(const KvRotateLaunch& L, hipStream_t stream) {
             : how == Turn::interleaved ? ((in_place ? L.turning : L.head_dim) + E - 1) / E
                                        : half + rest;
   p.per_token = p.units * (L.q.heads + L.k.heads);
-  p.tokens = 1;
-  p.part = p.per_token > 1024 * kRotThreads ? (p.per_token + 1023) / 1024 : kRotThreads;
+  // Few units: one a thread, so that all are under way.  Many: four a thread, and the
+  // stores with the non-temporal hint, since the chip's caches do not hold what comes out
+  // (8192 tokens, 168 MB in and out: 45 us without the hint, 27 with it).
+  const uint64_t units = uint64_t(L.n) * p.per_token;
+  const bool many = units > 256u * 8 * kRotThreads;
+  const int share = (many ? 4 : 1) * kRotThreads / p.per_token;
+  p.tokens = share < 1 ? 1 : share > 16 ? 16 : share;
+  p.part = p.per_token > 1024 * kRotThreads ? (p.per_token + 1023) / 1024 : many ? p.per_token : kRotThreads;
   const unsigned blocks = (L.n + p.tokens - 1) / p.tokens, parts = unsigned((p.per_token + p.part - 1) / p.part);
   const dim3 grid(blocks, parts);
   const size_t lds = size_t(p.tokens) * half * sizeof(float2);
-  return L.io_bf16 ? rotate_go<1>(p, how, grid, lds, stream) : rotate_go<0>(p, how, grid, lds, stream);
+  if (many) return L.io_bf16 ? rotate_go<1, 4>(p, how, grid, lds, stream) : rotate_go<0, 4>(p, how, grid, lds, stream);
+  return L.io_bf16 ? rotate_go<1, 1>(p, how, grid, lds, stream) : rotate_go<0, 1>(p, how, grid, lds, stream);
 }
 
 }  // namespace rwttt
