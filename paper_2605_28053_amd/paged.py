@@ -5,10 +5,13 @@ pages and the library's workspace.  A step is
 
     cache.extend(want)            # lengths -> pages and slots of the new rows
     per layer:
+        cache.rotate(rotary, q, k)  # rotary positions, in place
         cache.append(l, k, v)     # the new rows
         cache.select(l, q, keep)  # long contexts: the pages each query attends to
         cache.attend(l, q)        # one new token's attention per owner
     cache.commit()                # or cache.rollback(): the old lengths again
+
+and ``cache.gather(l, owners, positions)`` reads stored rows back.
 
 Nothing here waits for the GPU: lengths and slots stay on the device, and
 ``result`` holds the step's status there for whoever wants to read it.  Host
@@ -28,7 +31,10 @@ from . import _rwttt as R
 from . import _rwttt_kv as KV
 
 TORCH_DTYPE = {"f32": torch.float32, "bf16": torch.bfloat16, "fp8": torch.float8_e4m3fn}
-CODE = {"f32": R.RWTTT_F32, "bf16": R.RWTTT_BF16, "fp8": KV.RWTTT_FP8}
+CODE = {"f32": R.RWTTT_F32, "bf16": R.RWTTT_BF16, "fp8": KV.RWTTT_FP8, "fp4": KV.RWTTT_FP4}
+LAYOUT = {"half": KV.RWTTT_ROTARY_HALF, "interleaved": KV.RWTTT_ROTARY_INTERLEAVED}
+SCALING = {"plain": KV.RWTTT_ROTARY_PLAIN, "linear": KV.RWTTT_ROTARY_LINEAR, "base": KV.RWTTT_ROTARY_BASE,
+           "parts": KV.RWTTT_ROTARY_PARTS}
 
 
 def _check(status, where):
@@ -36,9 +42,40 @@ def _check(status, where):
         raise R.RwtttError(status, where)
 
 
+class Rotary:
+    """Rotary positions: which channels turn, how, and how fast.
+
+    ``turning`` channels of a head turn in pairs, i with i + turning / 2 (``layout``
+    "half") or 2 i with 2 i + 1 ("interleaved"), by base^(-2 i / turning) a position.
+    ``scaling`` stretches the context by ``factor``: "linear" slows all pairs, "base"
+    the slow ones the most, "parts" those of fewer than ``low`` turns over ``context``
+    positions and none of more than ``high``.  Turned channels are multiplied by ``gain``.
+    ``inverse()`` turns back: the gradient of the inputs from that of the outputs."""
+
+    def __init__(self, turning, base=10000.0, layout="half", scaling="plain", factor=1.0, low=1.0, high=32.0,
+                 context=8192.0, gain=1.0, device="cuda"):
+        if not 0 <= turning < 1 << 32:     # the binding would wrap it
+            raise ValueError(f"turning is {turning}")
+        if layout not in LAYOUT or scaling not in SCALING:
+            raise ValueError(f"layout is one of {list(LAYOUT)}, scaling of {list(SCALING)}")
+        units = KV.rwttt_kv_turns(turning, base, SCALING[scaling], factor, low, high, context)
+        self.turns = torch.tensor(units, dtype=torch.uint64).to(device)
+        self.turning, self.layout, self.gain = turning, layout, gain
+        self.struct = KV.make_rotary(turning, LAYOUT[layout], self.turns.data_ptr(), gain)
+
+    def inverse(self):
+        other = object.__new__(Rotary)
+        other.turns, other.turning, other.layout, other.gain = self.turns, self.turning, self.layout, self.gain
+        other.struct = KV.make_rotary(self.turning, LAYOUT[self.layout], self.turns.data_ptr(), self.gain,
+                                      not self.struct.inverse)
+        return other
+
+
 class PagedCache:
     """Pages of n_layers caches for n_owners requests, and one step's slots.
 
+    ``cache_dtype`` is "bf16", "f32" (with fp32 io), "fp8" or "fp4": e2m1 codes in blocks of
+    32 channels with a power of two each, whose pages are bytes.
     ``k_scale``, ``v_scale`` (8-bit caches) and ``bound_step`` (page selection)
     are numbers, or tensors [n_layers, n_kv_heads].  ``max_new`` is the most new
     rows that one step may add over all owners."""
@@ -49,7 +86,9 @@ class PagedCache:
         self.n_owners, self.n_layers, self.n_heads, self.n_kv_heads = n_owners, n_layers, n_heads, n_kv_heads
         self.head_dim, self.io_dtype, self.device = head_dim, io_dtype, device
         self.max_new = n_owners if max_new is None else max_new
-        shape = (n_pages, n_kv_heads, page_rows, head_dim)
+        fp4 = cache_dtype == "fp4"
+        shape = (n_pages, n_kv_heads, page_rows * head_dim * 17 // 32) if fp4 else (n_pages, n_kv_heads, page_rows, head_dim)
+        stored = torch.uint8 if fp4 else TORCH_DTYPE[cache_dtype]
 
         def i32(*size):
             return torch.zeros(size, dtype=torch.int32, device=device)
@@ -57,7 +96,7 @@ class PagedCache:
         def per_head(x):
             return torch.as_tensor(x, dtype=torch.float32, device=device).expand(n_layers, n_kv_heads).contiguous()
 
-        self.k, self.v = ([torch.empty(shape, dtype=TORCH_DTYPE[cache_dtype], device=device) for _ in range(n_layers)]
+        self.k, self.v = ([torch.empty(shape, dtype=stored, device=device) for _ in range(n_layers)]
                           for _ in range(2))
         self.table, self.ring = i32(n_owners, max_pages), torch.arange(n_pages, dtype=torch.int32, device=device)
         fp8 = cache_dtype == "fp8"
@@ -111,6 +150,32 @@ class PagedCache:
             self.positions.data_ptr(), self.max_new, self.result.data_ptr(), _stream()), "rwttt_kv_extend")
         self.open = True
 
+    def rotate(self, rotary, q=None, k=None, positions=None, q_out=None, k_out=None):
+        """Turn queries and keys [n, heads, head_dim] to their positions; in place unless q_out or k_out is given.
+
+        ``positions`` (int32 [n]) are the open step's, in slot order, if not given; tokens of
+        negative ones are left as they are.  Returns (q_out, k_out)."""
+        if q is None and k is None:
+            raise ValueError("queries or keys")
+        if (q is None and q_out is not None) or (k is None and k_out is not None):
+            raise ValueError("an output without its input")
+        self._here(rotary.turns, "the rotary's table")
+        q_out, k_out = q if q_out is None else q_out, k if k_out is None else k_out
+        n = len(k if q is None else q)
+        if positions is None:
+            if not self.open:
+                raise RuntimeError("no open step: give the positions")
+            if n > self.max_new:
+                raise ValueError("more rows than a step may add")
+            positions = self.positions[:n]
+        self._index(positions, n)
+        args = []
+        for t, heads, name in ((q, self.n_heads, "q"), (q_out, self.n_heads, "q_out"), (k, self.n_kv_heads, "k"),
+                               (k_out, self.n_kv_heads, "k_out")):
+            args += [0, 0] if t is None else [t.data_ptr(), self._rows(t, heads, name, n)]
+        _check(KV.rwttt_kv_rotate(self.kv, rotary.struct, positions.data_ptr(), n, *args, _stream()), "rwttt_kv_rotate")
+        return q_out, k_out
+
     def append(self, layer, k, v):
         """Store the open step's new rows: k, v [n, n_kv_heads, head_dim], n <= max_new, in slot order."""
         if not self.open:
@@ -121,6 +186,22 @@ class PagedCache:
             raise ValueError("k and v need the same number of rows, max_new at most")
         _check(KV.rwttt_kv_append(self.kv, layer, k.data_ptr(), k_stride, v.data_ptr(), v_stride,
                                   self.slots.data_ptr(), k.shape[0], _stream()), "rwttt_kv_append")
+
+    def gather(self, layer, owners, positions, k=None, v=None):
+        """The stored rows at ``positions`` of ``owners`` (int32 [n] each), as (k, v) [n, n_kv_heads, head_dim].
+
+        Rows of pairs that name none -- an open step's own rows are held -- stay as they are in
+        the given outputs, and are 0 in new ones."""
+        n = self._index(owners).numel()
+        self._index(positions, n)
+        self._counts(layer=layer)
+        shape, dtype = (n, self.n_kv_heads, self.head_dim), TORCH_DTYPE[self.io_dtype]
+        k = torch.zeros(shape, dtype=dtype, device=self.device) if k is None else k
+        v = torch.zeros(shape, dtype=dtype, device=self.device) if v is None else v
+        k_stride, v_stride = self._rows(k, self.n_kv_heads, "k", n), self._rows(v, self.n_kv_heads, "v", n)
+        _check(KV.rwttt_kv_gather(self.kv, layer, owners.data_ptr(), positions.data_ptr(), self.now().data_ptr(), n,
+                                  k.data_ptr(), k_stride, v.data_ptr(), v_stride, _stream()), "rwttt_kv_gather")
+        return k, v
 
     def select(self, layer, q, keep, first=1, last=2, rows=None, out=None):
         """Pages [n_owners, n_kv_heads, keep] that each listed owner's query attends to; -1 for the others."""

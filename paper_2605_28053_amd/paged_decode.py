@@ -3,7 +3,8 @@
     python -m paper_2605_28053_amd.paged_decode [--owners 8] [--layers 2] [--steps 200]
 
 Every layer of a step projects the owners' tokens to queries, keys and values,
-stores the keys and values in the owners' pages, attends -- over all rows, or
+turns queries and keys to their positions (``--rotary``), stores the keys and values
+in the owners' pages, attends -- over all rows, or
 over the selected pages once a context is longer than ``keep`` pages -- and
 passes the result through the MLP whose down-projection is the owners'
 fast-weight READ.  Requests come and go: an owner that has generated its tokens
@@ -18,7 +19,7 @@ import time
 import torch
 
 from . import _rwttt as R
-from .paged import PagedCache
+from .paged import PagedCache, Rotary
 
 
 class Model:
@@ -50,8 +51,10 @@ def norm(x):
 class Decoder:
     """A model with the state of n_owners requests: fast weights and pages."""
 
-    def __init__(self, model, n_owners, max_rows, page_rows=64, keep=0, cache_dtype=None, window=0, device="cuda"):
+    def __init__(self, model, n_owners, max_rows, page_rows=64, keep=0, cache_dtype=None, window=0, device="cuda",
+                 rotary=None):
         m = self.model = model
+        self.rotary = rotary
         self.n_owners, self.keep, self.window = n_owners, keep, window
         io = "f32" if m.dtype == torch.float32 else "bf16"
         max_pages = -(-max_rows // page_rows)
@@ -89,6 +92,8 @@ class Decoder:
         for l, w in enumerate(m.layers):
             qkv = (norm(x) @ w["qkv"]).view(n, m.n_heads + 2 * m.n_kv_heads, m.head_dim)
             q, k, v = qkv.split([m.n_heads, m.n_kv_heads, m.n_kv_heads], dim=1)
+            if self.rotary is not None:      # every owner has one new token, in owner order
+                self.cache.rotate(self.rotary, q, k)
             self.cache.append(l, k, v)
             pages = self.cache.select(l, q, self.keep) if self.keep else None
             a = self.cache.attend(l, q, pages=pages, window=self.window)
@@ -111,10 +116,12 @@ def main(argv=None):
     ap.add_argument("--layers", type=int, default=2)
     ap.add_argument("--steps", type=int, default=200)
     ap.add_argument("--keep", type=int, default=0, help="pages a query attends to (0: all)")
-    ap.add_argument("--cache", choices=["bf16", "fp8"], default="bf16")
+    ap.add_argument("--cache", choices=["bf16", "fp8", "fp4"], default="bf16")
+    ap.add_argument("--rotary", action="store_true", help="rotary positions in queries and keys")
     a = ap.parse_args(argv)
     model = Model(n_layers=a.layers)
-    dec = Decoder(model, a.owners, max_rows=a.steps + 64, keep=a.keep, cache_dtype=a.cache)
+    dec = Decoder(model, a.owners, max_rows=a.steps + 64, keep=a.keep, cache_dtype=a.cache,
+                  rotary=Rotary(model.head_dim) if a.rotary else None)
     tokens = torch.arange(a.owners, device="cuda") % model.vocab
     # request r ends after its own number of tokens: then its owner starts over, which
     # first returns the pages of the old one
