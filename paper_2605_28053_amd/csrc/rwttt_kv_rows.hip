@@ -17,8 +17,9 @@ namespace {
 //
 // An angle in turns is position * frequency, both whole numbers (the frequency
 // times 2^64), so the product modulo 2^64 is the exact place within a turn, at
-// position 1 as at 2^31; taken as a signed number, its conversion to fp32 keeps
-// 24 bits of small angles as well.
+// position 1 as at 2^31; taken as a signed number, its conversion keeps the bits
+// of small angles as well.  What fp32 drops of an angle is added to its sine and cosine,
+// to first order (below 2^-24 of a turn, so the second is below 2^-44).
 //
 // A block takes some tokens, computes their sines and cosines once into LDS --
 // heads share them -- and passes over its part of the rows.  A lane owns whole
@@ -67,8 +68,13 @@ struct RotateParams {
 // How the units of a head are laid out.
 enum class Turn { half, interleaved, pairs };   // pairs: HALF, one pair a unit
 
+// a b + c d with one product's rounding taken back, so that the sum's remains.
+__device__ __forceinline__ float two_products(float a, float b, float c, float d) {
+  const float p = c * d, sum = fmaf(a, b, p);
+  return __builtin_isfinite(p) ? sum + fmaf(c, d, -p) : sum;
+}
 __device__ __forceinline__ float2 turned(float2 x, float2 cs) {
-  return make_float2(fmaf(x.x, cs.x, -(x.y * cs.y)), fmaf(x.y, cs.x, x.x * cs.y));
+  return make_float2(two_products(x.x, cs.x, -x.y, cs.y), two_products(x.y, cs.x, x.x, cs.y));
 }
 
 template <int IO, Turn T, int U>
@@ -85,9 +91,12 @@ __global__ void __launch_bounds__(kRotThreads) kv_rotate_kernel(const RotatePara
   for (int i = threadIdx.x; i < nt * half; i += kRotThreads) {
     const int pos = p.positions[t0 + i / half];
     const int64_t place = int64_t(uint64_t(uint32_t(pos)) * p.turns[i % half]);
+    const double turn = double(place) * 0x1p-63;                // in half turns, [-1, 1]
+    const float near = float(turn), rest = float(turn - double(near)) * 3.14159265f;
     float s, c;
-    sincospif(float(place) * 0x1p-63f, &s, &c);
-    cs[i] = make_float2(c * p.gain, (p.inverse ? -s : s) * p.gain);
+    sincospif(near, &s, &c);
+    const float sin = fmaf(c, rest, s), cos = fmaf(-s, rest, c);
+    cs[i] = make_float2(cos * p.gain, (p.inverse ? -sin : sin) * p.gain);
   }
   bool waited = false;
   for (int i0 = threadIdx.x; i0 < total || !waited; i0 += U * kRotThreads) {

@@ -179,6 +179,28 @@ def test_rotation_depends_on_the_distance_alone():
     f.close()
 
 
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_infinities_and_nan_stay_in_their_pairs(io):
+    """A pair with an infinite channel becomes what the two products and their sum are; its
+    neighbours do not change."""
+    f = Rotor(2, 1, 64, 64, "half", io)
+    g = torch.Generator().manual_seed(6)
+    x = torch.randn((3, 2, 64), generator=g).to(DT[io])
+    clean = dev(x)
+    x[0, 0, 3], x[0, 1, 40], x[1, 0, 7], x[2, 1, 1], x[2, 1, 33] = math.inf, -math.inf, math.nan, math.inf, -math.inf
+    pos = [3, 100, 4321]
+    xd = dev(x)
+    for t in (clean, xd):
+        f(i32(pos), q=t, q_out=t)
+    torch.cuda.synchronize()
+    want, _ = f.ref(x, pos)
+    bad = ~torch.isfinite(want)
+    assert int(bad.sum()) == 8
+    assert torch.equal(xd.cpu().double()[bad].nan_to_num(0.5), want[bad].nan_to_num(0.5))
+    assert torch.equal(xd.cpu()[~bad], clean.cpu()[~bad])
+    f.close()
+
+
 def test_another_stream_and_a_graph():
     f = Rotor(8, 2, 128, 128)
     pos = i32([5, 9, -1])
