@@ -28,7 +28,8 @@ namespace {
 // of 16 bytes, a lane owns one pair.
 //
 // Bound by the bytes for a prefill: 8192 tokens of 32 + 8 heads of 128 channels in bf16
-// (168 MB in and out) take 27 us, 6.1 TB/s; a decode step of eight tokens 3.2 us.
+// (168 MB in and out) take 33 us, 5.1 TB/s, the rate of a copy, and 27 us where the last-level
+// cache still holds some of them; a decode step of eight tokens 3.1 us.
 
 constexpr int kRotThreads = 256;
 
@@ -58,23 +59,40 @@ template <int IO> struct IoRow {           // 16 bytes of io
   }
 };
 
+// Division by a number known to the host: floor(2^32 / by) gives the quotient or one less.
+struct Divider {
+  uint32_t by, magic;
+  __device__ __forceinline__ uint32_t operator()(uint32_t x, uint32_t& rest) const {
+    uint32_t q = __umulhi(x, magic);
+    rest = x - q * by;
+    if (rest >= by) {
+      ++q;
+      rest -= by;
+    }
+    return q;
+  }
+};
+Divider divider(uint32_t by) { return {by, uint32_t((uint64_t(1) << 32) / by - (by == 1))}; }
+
 struct RotateParams {
   KvRotateLaunch L;
   int tokens;              // of a block
-  int units;               // of a head: what one lane takes at a time
+  Divider units;           // of a head: what one lane takes at a time
   int per_token, part;     // units of a token, of a block's part of them
+  Divider whole;           // per_token
 };
 
 // How the units of a head are laid out.
 enum class Turn { half, interleaved, pairs };   // pairs: HALF, one pair a unit
 
-// a b + c d with one product's rounding taken back, so that the sum's remains.
-__device__ __forceinline__ float two_products(float a, float b, float c, float d) {
+// a b + c d, of fp32 io with one product's rounding taken back, so that the sum's remains.
+template <int IO> __device__ __forceinline__ float two_products(float a, float b, float c, float d) {
   const float p = c * d, sum = fmaf(a, b, p);
+  if constexpr (IO) return sum;
   return __builtin_isfinite(p) ? sum + fmaf(c, d, -p) : sum;
 }
-__device__ __forceinline__ float2 turned(float2 x, float2 cs) {
-  return make_float2(two_products(x.x, cs.x, -x.y, cs.y), two_products(x.y, cs.x, x.x, cs.y));
+template <int IO> __device__ __forceinline__ float2 turned(float2 x, float2 cs) {
+  return make_float2(two_products<IO>(x.x, cs.x, -x.y, cs.y), two_products<IO>(x.y, cs.x, x.x, cs.y));
 }
 
 template <int IO, Turn T, int U>
@@ -114,10 +132,11 @@ __global__ void __launch_bounds__(kRotThreads) kv_rotate_kernel(const RotatePara
       const int i = i0 + j * kRotThreads;
       w.x = -1;
       if (i >= total) continue;
-      const int t = i / span, u = u0 + i % span;
+      uint32_t u = i, x;                 // of one token a part of its units, of several all
+      const int t = rp.tokens > 1 ? int(rp.whole(i, u)) : 0;
       if (p.positions[t0 + t] < 0) continue;
-      int h = u / rp.units;
-      w.x = u % rp.units;
+      int h = int(rp.units(u0 + u, x));
+      w.x = int(x);
       const bool is_k = h >= p.q.heads;
       const KvTurnRows& rows = is_k ? p.k : p.q;
       h -= is_k ? p.q.heads : 0;
@@ -146,8 +165,8 @@ __global__ void __launch_bounds__(kRotThreads) kv_rotate_kernel(const RotatePara
           IoRow<IO> ra, rb;
 #pragma unroll
           for (int e = 0; e < E; e += 2) {
-            const float2 y0 = turned(make_float2(w.a.get(e), w.b.get(e)), w.at[w.x * E + e]);
-            const float2 y1 = turned(make_float2(w.a.get(e + 1), w.b.get(e + 1)), w.at[w.x * E + e + 1]);
+            const float2 y0 = turned<IO>(make_float2(w.a.get(e), w.b.get(e)), w.at[w.x * E + e]);
+            const float2 y1 = turned<IO>(make_float2(w.a.get(e + 1), w.b.get(e + 1)), w.at[w.x * E + e + 1]);
             ra.put_pair(e / 2, y0.x, y1.x);
             rb.put_pair(e / 2, y0.y, y1.y);
           }
@@ -161,14 +180,14 @@ __global__ void __launch_bounds__(kRotThreads) kv_rotate_kernel(const RotatePara
         for (int e = 0; e < E / 2; ++e) {
           const int k = w.x * (E / 2) + e;
           if (k < half) {
-            const float2 y = turned(make_float2(w.a.get(2 * e), w.a.get(2 * e + 1)), w.at[k]);
+            const float2 y = turned<IO>(make_float2(w.a.get(2 * e), w.a.get(2 * e + 1)), w.at[k]);
             w.a.put_pair(e, y.x, y.y);
           }
         }
         w.a.template store<HINT>(w.dst + w.x * 16);
       } else {
         if (w.x < half) {
-          const float2 y = turned(w.pair, w.at[w.x]);
+          const float2 y = turned<IO>(w.pair, w.at[w.x]);
           M::put(w.dst, w.x, y.x);
           M::put(w.dst, w.x + half, y.y);
         } else {
@@ -185,9 +204,11 @@ __global__ void __launch_bounds__(kRotThreads) kv_rotate_kernel(const RotatePara
 //
 // A wave takes one kv head of a run of rows: LPR lanes hold a row, 16 bytes of
 // output each, and the loads of its keys and values are in flight at once behind
-// the chain owner -> length and page.  Bound by the bytes, of which the output is the
-// most: 48700 rows of eight heads of 128 channels from 4 bits to bf16 (253 MB) take
-// 42 us, 6.0 TB/s, with non-temporal stores, 75 without; 500 rows 3.4 us.
+// the chain owner -> length and page.  A block's waves take runs behind one another, since
+// the powers of a page's rows share lines (with the waves on four heads of the same rows
+// 73 MB are fetched instead of 54).  Bound by the bytes, of which the output is the most:
+// 48700 rows of eight heads of 128 channels from 4 bits to bf16 (253 MB) take 40 us, 6.2
+// TB/s, with non-temporal stores, 75 without; 500 rows 3.3 us.
 
 struct GatherParams {
   KvGatherLaunch L;
@@ -199,9 +220,9 @@ __global__ void __launch_bounds__(256) kv_gather_kernel(const GatherParams gp) {
   const KvGatherLaunch& p = gp.L;
   using Row = CachedRow<IO, CT, D>;
   constexpr int IOB = IO ? 2 : 4, E = Row::E, LPR = D / E, RPI = 64 / LPR;
-  const int lane = threadIdx.x & 63, unit = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int H = p.s.kv_heads, shift = p.s.page_shift, P = 1 << shift;
-  const int h = unit % H, n = int(p.n), t0 = unit / H * gp.run, t1 = min(n, t0 + gp.run);
+  const int h = blockIdx.x % H, n = int(p.n), t0 = (blockIdx.x / H * 4 + wave) * gp.run, t1 = min(n, t0 + gp.run);
   if (t0 >= n) return;
   const int sub = lane / LPR, piece = lane % LPR, most = p.s.max_pages << shift;
 
@@ -240,12 +261,11 @@ __global__ void __launch_bounds__(256) kv_gather_kernel(const GatherParams gp) {
 template <int IO, int CT, int D> hipError_t gather_go(GatherParams p, hipStream_t stream) {
   constexpr int RPI = 64 * (IO ? 8 : 4) / D;
   const uint64_t rows = uint64_t(p.L.n) * p.L.s.kv_heads;
-  // two loads of rows a wave where that still makes eight waves a SIMD (256 MB of 128
-  // channels in bf16 42.4 us, in fp32 104; with one 43.3 and 107, with four 43.4 and 104)
+  // two loads of rows a wave where that still makes eight waves a SIMD (253 MB of 128
+  // channels in bf16 42.4 us, with one 43.3, with four 43.4)
   const bool many = rows >= 8192u * 2 * RPI;
   p.run = many ? 2 * RPI : RPI;
-  const uint64_t units = uint64_t((p.L.n + p.run - 1) / p.run) * p.L.s.kv_heads;
-  const dim3 grid(unsigned((units + 3) / 4)), block(256);
+  const dim3 grid(unsigned((p.L.n + 4 * p.run - 1) / (4 * p.run) * p.L.s.kv_heads)), block(256);
   if (many) hipLaunchKernelGGL((kv_gather_kernel<IO, CT, D, 2>), grid, block, 0, stream, p);
   else hipLaunchKernelGGL((kv_gather_kernel<IO, CT, D, 1>), grid, block, 0, stream, p);
   return hipGetLastError();
@@ -286,18 +306,21 @@ hipError_t launch_kv_rotate(const KvRotateLaunch& L, hipStream_t stream) {
   const bool in_place = (!L.q.heads || L.q.in == L.q.out) && (!L.k.heads || L.k.in == L.k.out);
   // in place the channels that do not turn are where they belong
   const int rest = in_place ? 0 : L.head_dim - L.turning;
-  p.units = how == Turn::half          ? half / E + rest / E
-            : how == Turn::interleaved ? ((in_place ? L.turning : L.head_dim) + E - 1) / E
-                                       : half + rest;
-  p.per_token = p.units * (L.q.heads + L.k.heads);
+  const int of_head = how == Turn::half          ? half / E + rest / E
+                      : how == Turn::interleaved ? ((in_place ? L.turning : L.head_dim) + E - 1) / E
+                                                 : half + rest;
+  p.units = divider(uint32_t(of_head));
+  p.per_token = of_head * (L.q.heads + L.k.heads);
+  p.whole = divider(uint32_t(p.per_token));
   // Few units: one a thread, so that all are under way.  Many: four a thread, and the
   // stores with the non-temporal hint, since the chip's caches do not hold what comes out
-  // (8192 tokens, 168 MB in and out: 45 us without the hint, 27 with it).
+  // (8192 tokens, 168 MB in and out: 45 us without the hint, 27 to 33 with it).
   const uint64_t units = uint64_t(L.n) * p.per_token;
   const bool many = units > 256u * 8 * kRotThreads;
   const int share = (many ? 4 : 1) * kRotThreads / p.per_token;
   p.tokens = share < 1 ? 1 : share > 16 ? 16 : share;
   p.part = p.per_token > 1024 * kRotThreads ? (p.per_token + 1023) / 1024 : many ? p.per_token : kRotThreads;
+  if (p.tokens > 1) p.part = p.per_token;
   const unsigned blocks = (L.n + p.tokens - 1) / p.tokens, parts = unsigned((p.per_token + p.part - 1) / p.part);
   const dim3 grid(blocks, parts);
   const size_t lds = size_t(p.tokens) * half * sizeof(float2);
