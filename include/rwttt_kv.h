@@ -61,6 +61,7 @@ extern "C" {
  *   bytes a row, channel 2 i in the low half of byte i; then, for each block of 32
  *   channels in turn, one byte E a row.  A code is a sign and one of 0, 1/2, 1, 3/2,
  *   2, 3, 4, 6; its value is that times 2^(E - 127), and NaN for all 32 where E is 255.
+ *   rwttt_kv_append writes E from 2 to 252, or 255; others' values are not specified.
  */
 #define RWTTT_FP8  2
 #define RWTTT_FP4  4

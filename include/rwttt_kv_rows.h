@@ -64,10 +64,12 @@ rwttt_status rwttt_kv_turns(uint32_t turning, double base, int32_t scaling, doub
  * q_out and k_out, which may be q and k themselves with the same stride.  A token
  * of negative position (the -1 of a padded one) is skipped: its rows of the
  * outputs are left as they were.  q with q_out, or k with k_out, may be NULL.
- * Angles' sines and cosines and the products are fp32, the results rounded once.
+ * Angles' sines and cosines and the products are fp32, the results rounded once; an
+ * infinite channel makes its pair what the two products and their sum are.
  * Needs no buffer of the handle but its shape; n = 0 launches nothing.  One launch.
  * Errors: RWTTT_E_INVALID for a bad rotary, null or misaligned pointers, a bad
- * stride, an output that overlaps an input or the other output other than as said. */
+ * stride, an output that overlaps an input or the other output other than as said
+ * (rows of different strides count as overlapping where the spans of all n meet). */
 rwttt_status rwttt_kv_rotate(rwttt_kv* kv, const rwttt_kv_rotary* rotary, const int32_t* positions, uint32_t n,
                              const void* q, uint64_t q_stride, void* q_out, uint64_t q_out_stride,
                              const void* k, uint64_t k_stride, void* k_out, uint64_t k_out_stride, void* stream);
@@ -79,7 +81,8 @@ rwttt_status rwttt_kv_rotate(rwttt_kv* kv, const rwttt_kv_rotary* rotary, const 
  * outside [0, n_owners) or whose position is outside [0, lengths[owner]) is
  * skipped: its rows of k and v are left as they were.  k or v may be NULL.
  * n = 0 launches nothing.  One launch.
- * Errors: RWTTT_E_INVALID as above, or without k, v or table in the handle. */
+ * Errors: RWTTT_E_INVALID as above, for outputs that overlap, or without k, v or table
+ * in the handle. */
 rwttt_status rwttt_kv_gather(rwttt_kv* kv, uint32_t layer, const int32_t* owners, const int32_t* positions,
                              const int32_t* lengths, uint32_t n, void* k, uint64_t k_stride, void* v,
                              uint64_t v_stride, void* stream);
