@@ -48,9 +48,9 @@ typedef struct rwttt_kv_rotary {
  *                        kept in [0, 1], w_i (r + (1 - r) / factor)
  * Writes turns[turning / 2] (host memory), to be copied to the device.  Host only.
  * Any other table of frequencies may be used as well.
- * RWTTT_E_INVALID: turning 0 or odd, base not above 1, a number that is not finite, a
- * factor not above 0 (unless PLAIN), turning 2 with BASE, context not above 0 or high not
- * above low with PARTS. */
+ * RWTTT_E_INVALID: turning 0, odd or above 256, base not above 1, a number that
+ * is not finite, a factor not above 0 (unless PLAIN), turning 2 with BASE, context not
+ * above 0 or high not above low with PARTS. */
 #define RWTTT_ROTARY_PLAIN  0
 #define RWTTT_ROTARY_LINEAR 1
 #define RWTTT_ROTARY_BASE   2

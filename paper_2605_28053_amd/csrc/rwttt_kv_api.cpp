@@ -306,7 +306,8 @@ rwttt_status rwttt_kv_attend(rwttt_kv* kv, uint32_t layer, const void* q, uint64
 
 rwttt_status rwttt_kv_turns(uint32_t turning, double base, int32_t scaling, double factor, double low, double high,
                             double context, uint64_t* turns) {
-  if (!turns || turning == 0 || turning % 2 || !std::isfinite(base) || base <= 1.0) return RWTTT_E_INVALID;
+  if (!turns || turning == 0 || turning % 2 || turning > 256 || !std::isfinite(base) || base <= 1.0)
+    return RWTTT_E_INVALID;
   if (scaling < RWTTT_ROTARY_PLAIN || scaling > RWTTT_ROTARY_PARTS) return RWTTT_E_INVALID;
   if (scaling != RWTTT_ROTARY_PLAIN && (!std::isfinite(factor) || factor <= 0.0)) return RWTTT_E_INVALID;
   if (scaling == RWTTT_ROTARY_BASE && turning == 2) return RWTTT_E_INVALID;

@@ -319,6 +319,7 @@ hipError_t launch_kv_rotate(const KvRotateLaunch& L, hipStream_t stream) {
   const bool many = units > 256u * 8 * kRotThreads;
   const int share = (many ? 4 : 1) * kRotThreads / p.per_token;
   p.tokens = share < 1 ? 1 : share > 16 ? 16 : share;
+  if (L.n > (1u << 23) && p.tokens < 2) p.tokens = 2;          // a launch's threads stay below 2^32
   p.part = p.per_token > 1024 * kRotThreads ? (p.per_token + 1023) / 1024 : many ? p.per_token : kRotThreads;
   if (p.tokens > 1) p.part = p.per_token;
   const unsigned blocks = (L.n + p.tokens - 1) / p.tokens, parts = unsigned((p.per_token + p.part - 1) / p.part);

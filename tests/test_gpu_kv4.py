@@ -198,6 +198,20 @@ def test_attend_head_layouts(H, G, io):
     c.close()
 
 
+@pytest.mark.parametrize("G", [5, 8, 16, 20])
+@pytest.mark.parametrize("D", [128, 256])
+def test_attend_the_most_owners_and_the_widest_rows(D, G):
+    """4096 owners: the most LDS a call asks for."""
+    rng = random.Random(8)
+    lens = [rng.choice([0, 1, 3, 16]) for _ in range(4096)]
+    lens[2000] = 700
+    c = Cache4(lens, H=1, G=G, D=D, page=16, io="bf16", seed=1, poison=False)
+    got = c.attend()
+    for r in list(range(0, 4096, 201)) + [2000, 4095]:
+        c.check(got, r)
+    c.close()
+
+
 @pytest.mark.parametrize("io", ["bf16", "f32"])
 @pytest.mark.parametrize("D", [64, 128, 256])
 def test_attend_long_rows_are_split_and_joined(io, D):

@@ -185,6 +185,7 @@ def test_frequencies_by_hand():
     (0, 1e4), (3, 1e4), (64, 1.0), (64, math.nan), (64, math.inf), (64, -5.0), (64, 1e4, 4), (64, 1e4, -1),
     (64, 1e4, 1, 0.0), (64, 1e4, 1, -2.0), (64, 1e4, 1, math.nan), (64, 1e4, 2, math.inf), (2, 1e4, 2, 4.0),
     (64, 1e4, 3, 4.0, 1.0, 1.0, 100.0), (64, 1e4, 3, 4.0, 2.0, 1.0, 100.0), (64, 1e4, 3, 4.0, 1.0, 32.0, 0.0),
+    (258, 1e4),
     (64, 1e4, 3, 4.0, math.nan, 32.0, 100.0), (64, 1e4, 3, 4.0, 1.0, math.inf, 100.0), (64, 1e4, 3, 4.0, 1.0, 32.0, math.nan)])
 def test_frequencies_refuse(args):
     with pytest.raises(R.RwtttError) as e:
