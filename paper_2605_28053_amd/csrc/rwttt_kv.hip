@@ -1287,213 +1287,213 @@ __global__ void __launch_bounds__(kAttThreads, blocks_a_cu(IO, CT, D)) kv_attend
                       last_page, t0, t1};
       attend_rows4<IO, D, NT_HINT, TG>(p, at4, ap.scale_log2, owner, head0, heads, m, l, acc);
     } else {
-    auto locate = [&](int t) {
-      TileAt<NT> at;
+      auto locate = [&](int t) {
+        TileAt<NT> at;
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        const int row0 = base + t * KT + j * 16;
-        int lp = row0 >> shift;
-        at.off[j] = row0 & (P - 1);
-        bool none = false;
-        if (p.pages) {
-          none = lp >= held;
-          lp = list[min(lp, held - 1)];
-          none = none || unsigned(lp) > unsigned(last_page);
+        for (int j = 0; j < NT; ++j) {
+          const int row0 = base + t * KT + j * 16;
+          int lp = row0 >> shift;
+          at.off[j] = row0 & (P - 1);
+          bool none = false;
+          if (p.pages) {
+            none = lp >= held;
+            lp = list[min(lp, held - 1)];
+            none = none || unsigned(lp) > unsigned(last_page);
+          }
+          const int pos = (lp << shift) + at.off[j];
+          at.from[j] = clampi(least - pos, 0, 16);
+          at.to[j] = none ? 0 : clampi(len - pos, 0, 16);
+          at.page[j] = min(uint32_t(table[clampi(lp, 0, last_page)]), uint32_t(p.s.n_pages - 1));
         }
-        const int pos = (lp << shift) + at.off[j];
-        at.from[j] = clampi(least - pos, 0, 16);
-        at.to[j] = none ? 0 : clampi(len - pos, 0, 16);
-        at.page[j] = min(uint32_t(table[clampi(lp, 0, last_page)]), uint32_t(p.s.n_pages - 1));
-      }
-      return at;
-    };
+        return at;
+      };
 
-    // queries: the lane's column is one of them; piece s of its channels feeds PER operands
-    constexpr int PER = F ? 1 : S::KE / 8, QN = F ? D / 16 : D / 32, QW = F || IO ? 4 : 8;
-    const char* q_at = static_cast<const char*>(p.q) +
-                       (size_t(owner) * p.q_stride + (size_t(h) * G + head0 + (c < heads ? c : 0)) * D) * (IO ? 2 : 4);
-    uint32_t qw[QN][QW];
+      // queries: the lane's column is one of them; piece s of its channels feeds PER operands
+      constexpr int PER = F ? 1 : S::KE / 8, QN = F ? D / 16 : D / 32, QW = F || IO ? 4 : 8;
+      const char* q_at = static_cast<const char*>(p.q) +
+                         (size_t(owner) * p.q_stride + (size_t(h) * G + head0 + (c < heads ? c : 0)) * D) * (IO ? 2 : 4);
+      uint32_t qw[QN][QW];
 #pragma unroll
-    for (int s = 0; s < QN; ++s) {
-      const int ch = S::key_channel(s / PER, g) + (s % PER) * 8;
+      for (int s = 0; s < QN; ++s) {
+        const int ch = S::key_channel(s / PER, g) + (s % PER) * 8;
 #pragma unroll
-      for (int j = 0; j < QW; j += 4) load_words<4>(q_at + ch * (IO ? 2 : 4) + j * 4, &qw[s][j]);
-    }
-    const float to_log2 = ap.scale_log2 * (CT == RWTTT_FP8 && p.k_scale ? p.k_scale[h] : 1.f);
-
-    uint32_t kw[NT][S::KW][4];
-    uint32_t vw[S::NE][S::VR][S::VW];
-    // row of a half that the lane loads: keys, one a lane; values, VR in turn
-    const int k_half = NT == 2 ? c >> 3 : 0, v_half = NT == 2 ? g >> 1 : 0;
-    auto half_of = [&](const TileAt<NT>& at, const void* cache, int half) {
-      const uint32_t page = NT == 2 && half ? at.page[NT - 1] : at.page[0];
-      const int off = NT == 2 && half ? at.off[NT - 1] : at.off[0];
-      return static_cast<const char*>(cache) + ((size_t(page) * H + h) * P + off) * size_t(D * S::B);
-    };
-    auto load_keys = [&](const TileAt<NT>& at) {
-      const char* src = half_of(at, p.k, k_half);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const int rr = NT == 2 ? ((c >> 2) & 1) * 8 + t * 4 + (c & 3) : c;
-#pragma unroll
-        for (int s = 0; s < S::KW; ++s) load_words<4, NT_HINT>(src + (rr * D + S::key_channel(s, g)) * S::B, kw[t][s]);
+        for (int j = 0; j < QW; j += 4) load_words<4>(q_at + ch * (IO ? 2 : 4) + j * 4, &qw[s][j]);
       }
-    };
-    auto load_values = [&](const TileAt<NT>& at) {
-      const char* src = half_of(at, p.v, v_half);
+      const float to_log2 = ap.scale_log2 * (CT == RWTTT_FP8 && p.k_scale ? p.k_scale[h] : 1.f);
+
+      uint32_t kw[NT][S::KW][4];
+      uint32_t vw[S::NE][S::VR][S::VW];
+      // row of a half that the lane loads: keys, one a lane; values, VR in turn
+      const int k_half = NT == 2 ? c >> 3 : 0, v_half = NT == 2 ? g >> 1 : 0;
+      auto half_of = [&](const TileAt<NT>& at, const void* cache, int half) {
+        const uint32_t page = NT == 2 && half ? at.page[NT - 1] : at.page[0];
+        const int off = NT == 2 && half ? at.off[NT - 1] : at.off[0];
+        return static_cast<const char*>(cache) + ((size_t(page) * H + h) * P + off) * size_t(D * S::B);
+      };
+      auto load_keys = [&](const TileAt<NT>& at) {
+        const char* src = half_of(at, p.k, k_half);
 #pragma unroll
-      for (int e = 0; e < S::NE; ++e)
+        for (int t = 0; t < NT; ++t) {
+          const int rr = NT == 2 ? ((c >> 2) & 1) * 8 + t * 4 + (c & 3) : c;
 #pragma unroll
-        for (int k = 0; k < S::VR; ++k) {
-          const int rr = NT == 2 ? (g & 1) * 8 + k : g * 4 + k;
-          load_words<S::VW, NT_HINT>(src + (rr * D + S::value_channel(e, c)) * S::B, vw[e][k]);
+          for (int s = 0; s < S::KW; ++s) load_words<4, NT_HINT>(src + (rr * D + S::key_channel(s, g)) * S::B, kw[t][s]);
         }
-    };
+      };
+      auto load_values = [&](const TileAt<NT>& at) {
+        const char* src = half_of(at, p.v, v_half);
+#pragma unroll
+        for (int e = 0; e < S::NE; ++e)
+#pragma unroll
+          for (int k = 0; k < S::VR; ++k) {
+            const int rr = NT == 2 ? (g & 1) * 8 + k : g * 4 + k;
+            load_words<S::VW, NT_HINT>(src + (rr * D + S::value_channel(e, c)) * S::B, vw[e][k]);
+          }
+      };
 
-    TileAt<NT> at = locate(min(t0, seg1 - 1)), next = at;
-    // With the condition the compiler keeps a second set of registers and loads the
-    // next tile while this one is in use: 347 against 373 us for 16 owners of 8500
-    // rows, head dim 256, fp32.  Three terms of a query leave no room for it.
-    constexpr bool kSecondSet = IO || CT != RWTTT_BF16;
-    if (!kSecondSet || t0 < t1) {
-      load_keys(at);
-      load_values(at);
-    }
-    bf16x8_t q[F ? 1 : NQ][F ? 1 : QN];
-    f32x4_t qf[F ? QN : 1];
-#pragma unroll
-    for (int s = 0; s < QN; ++s) {
-#pragma unroll
-      for (int j = 0; j < QW; ++j) qw[s][j] = c < heads ? qw[s][j] : 0u;
-      if constexpr (F) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) qf[s][j] = __uint_as_float(qw[s][j]);
-      } else if constexpr (IO) {
-        q[0][s] = as_bf16x8(qw[s]);
-      } else {
-        float f[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(qw[s][j]);
-        bf16x8_t terms[NQ];
-        split_bf16<NQ>(f, terms);
-#pragma unroll
-        for (int k = 0; k < NQ; ++k) q[k][s] = terms[k];
+      TileAt<NT> at = locate(min(t0, seg1 - 1)), next = at;
+      // With the condition the compiler keeps a second set of registers and loads the
+      // next tile while this one is in use: 347 against 373 us for 16 owners of 8500
+      // rows, head dim 256, fp32.  Three terms of a query leave no room for it.
+      constexpr bool kSecondSet = IO || CT != RWTTT_BF16;
+      if (!kSecondSet || t0 < t1) {
+        load_keys(at);
+        load_values(at);
       }
-    }
-    for (int t = t0; t < t1; ++t) {
-      const bool more = t + 1 < t1;
-      if (more) next = locate(t + 1);
-
-      // scores: s[j] belongs to the tile's row g * VR + j
-      float s[S::VR];
+      bf16x8_t q[F ? 1 : NQ][F ? 1 : QN];
+      f32x4_t qf[F ? QN : 1];
 #pragma unroll
-      for (int k = 0; k < NT; ++k) {
-        f32x4_t sc = {0.f, 0.f, 0.f, 0.f};
+      for (int s = 0; s < QN; ++s) {
+#pragma unroll
+        for (int j = 0; j < QW; ++j) qw[s][j] = c < heads ? qw[s][j] : 0u;
         if constexpr (F) {
 #pragma unroll
-          for (int a = 0; a < D / 16; ++a)
-#pragma unroll
-            for (int b = 0; b < 4; ++b)
-              sc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kw[k][a][b]), qf[a][b], sc, 0, 0, 0);
+          for (int j = 0; j < 4; ++j) qf[s][j] = __uint_as_float(qw[s][j]);
+        } else if constexpr (IO) {
+          q[0][s] = as_bf16x8(qw[s]);
         } else {
+          float f[8];
 #pragma unroll
-          for (int a = 0; a < D / 32; ++a) {
-            bf16x8_t key;
-            if constexpr (CT == RWTTT_BF16) {
-              key = as_bf16x8(kw[k][a]);
-            } else {
+          for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(qw[s][j]);
+          bf16x8_t terms[NQ];
+          split_bf16<NQ>(f, terms);
+#pragma unroll
+          for (int k = 0; k < NQ; ++k) q[k][s] = terms[k];
+        }
+      }
+      for (int t = t0; t < t1; ++t) {
+        const bool more = t + 1 < t1;
+        if (more) next = locate(t + 1);
+
+        // scores: s[j] belongs to the tile's row g * VR + j
+        float s[S::VR];
+#pragma unroll
+        for (int k = 0; k < NT; ++k) {
+          f32x4_t sc = {0.f, 0.f, 0.f, 0.f};
+          if constexpr (F) {
+#pragma unroll
+            for (int a = 0; a < D / 16; ++a)
+#pragma unroll
+              for (int b = 0; b < 4; ++b)
+                sc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kw[k][a][b]), qf[a][b], sc, 0, 0, 0);
+          } else {
+#pragma unroll
+            for (int a = 0; a < D / 32; ++a) {
+              bf16x8_t key;
+              if constexpr (CT == RWTTT_BF16) {
+                key = as_bf16x8(kw[k][a]);
+              } else {
+                uint32_t wd[4];
+#pragma unroll
+                for (int b = 0; b < 4; ++b) wd[b] = fp8_pair(kw[k][a / 2][(a & 1) * 2 + b / 2], b & 1);
+                key = as_bf16x8(wd);
+              }
+#pragma unroll
+              for (int b = NQ - 1; b >= 0; --b)
+                sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[b][a], sc, 0, 0, 0);
+            }
+          }
+#pragma unroll
+          for (int b = 0; b < 4; ++b) s[k * 4 + b] = sc[b] * to_log2;
+        }
+        if (more) load_keys(next);
+
+        bool whole = true;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) whole = whole && at.from[j] == 0 && at.to[j] == 16;
+        // the lane's rows of its half that count
+        const int from = (v_half ? at.from[NT - 1] : at.from[0]) - (NT == 2 ? (g & 1) * 8 : g * 4);
+        const int to = (v_half ? at.to[NT - 1] : at.to[0]) - (NT == 2 ? (g & 1) * 8 : g * 4);
+        if (!whole) {
+#pragma unroll
+          for (int j = 0; j < S::VR; ++j) s[j] = j >= from && j < to ? s[j] : -INFINITY;
+        }
+        float top = s[0];
+#pragma unroll
+        for (int j = 1; j < S::VR; ++j) top = fmaxf(top, s[j]);
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (__any(top > m)) {
+          const float up = fmaxf(m, top), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - up);
+          m = up;
+          l *= f;
+#pragma unroll
+          for (int a = 0; a < S::NA; ++a) acc[a] *= f;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+        float pr[S::VR];
+#pragma unroll
+        for (int j = 0; j < S::VR; ++j) {
+          pr[j] = __builtin_amdgcn_exp2f(s[j] - ref);
+          l += pr[j];
+        }
+        if (!whole) {                      // what lies behind an owner's rows may be anything
+#pragma unroll
+          for (int e = 0; e < S::NE; ++e)
+#pragma unroll
+            for (int j = 0; j < S::VR; ++j)
+#pragma unroll
+              for (int b = 0; b < S::VW; ++b) vw[e][j][b] = j >= from && j < to ? vw[e][j][b] : 0u;
+        }
+        if constexpr (F) {
+#pragma unroll
+          for (int e = 0; e < S::NE; ++e)
+#pragma unroll
+            for (int a = 0; a < 4; ++a)
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                acc[e * 4 + a] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vw[e][j][a]), pr[j],
+                                                                      acc[e * 4 + a], 0, 0, 0);
+        } else {
+          bf16x8_t pt[NP];
+          split_bf16<NP>(pr, pt);
+#pragma unroll
+          for (int e = 0; e < S::NE; ++e)
+#pragma unroll
+            for (int a = 0; a < S::VE; ++a) {
               uint32_t wd[4];
 #pragma unroll
-              for (int b = 0; b < 4; ++b) wd[b] = fp8_pair(kw[k][a / 2][(a & 1) * 2 + b / 2], b & 1);
-              key = as_bf16x8(wd);
-            }
-#pragma unroll
-            for (int b = NQ - 1; b >= 0; --b)
-              sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[b][a], sc, 0, 0, 0);
-          }
-        }
-#pragma unroll
-        for (int b = 0; b < 4; ++b) s[k * 4 + b] = sc[b] * to_log2;
-      }
-      if (more) load_keys(next);
-
-      bool whole = true;
-#pragma unroll
-      for (int j = 0; j < NT; ++j) whole = whole && at.from[j] == 0 && at.to[j] == 16;
-      // the lane's rows of its half that count
-      const int from = (v_half ? at.from[NT - 1] : at.from[0]) - (NT == 2 ? (g & 1) * 8 : g * 4);
-      const int to = (v_half ? at.to[NT - 1] : at.to[0]) - (NT == 2 ? (g & 1) * 8 : g * 4);
-      if (!whole) {
-#pragma unroll
-        for (int j = 0; j < S::VR; ++j) s[j] = j >= from && j < to ? s[j] : -INFINITY;
-      }
-      float top = s[0];
-#pragma unroll
-      for (int j = 1; j < S::VR; ++j) top = fmaxf(top, s[j]);
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      if (__any(top > m)) {
-        const float up = fmaxf(m, top), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - up);
-        m = up;
-        l *= f;
-#pragma unroll
-        for (int a = 0; a < S::NA; ++a) acc[a] *= f;
-      }
-      const float ref = m == -INFINITY ? 0.f : m;
-      float pr[S::VR];
-#pragma unroll
-      for (int j = 0; j < S::VR; ++j) {
-        pr[j] = __builtin_amdgcn_exp2f(s[j] - ref);
-        l += pr[j];
-      }
-      if (!whole) {                      // what lies behind an owner's rows may be anything
-#pragma unroll
-        for (int e = 0; e < S::NE; ++e)
-#pragma unroll
-          for (int j = 0; j < S::VR; ++j)
-#pragma unroll
-            for (int b = 0; b < S::VW; ++b) vw[e][j][b] = j >= from && j < to ? vw[e][j][b] : 0u;
-      }
-      if constexpr (F) {
-#pragma unroll
-        for (int e = 0; e < S::NE; ++e)
-#pragma unroll
-          for (int a = 0; a < 4; ++a)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              acc[e * 4 + a] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vw[e][j][a]), pr[j],
-                                                                    acc[e * 4 + a], 0, 0, 0);
-      } else {
-        bf16x8_t pt[NP];
-        split_bf16<NP>(pr, pt);
-#pragma unroll
-        for (int e = 0; e < S::NE; ++e)
-#pragma unroll
-          for (int a = 0; a < S::VE; ++a) {
-            uint32_t wd[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              if constexpr (CT == RWTTT_BF16) {
-                wd[j] = __builtin_amdgcn_perm(vw[e][2 * j + 1][a / 2], vw[e][2 * j][a / 2],
-                                              a & 1 ? 0x07060302u : 0x05040100u);
-              } else {
-                wd[j] = fp8_pair(__builtin_amdgcn_perm(vw[e][2 * j + 1][a / 4], vw[e][2 * j][a / 4],
-                                                       a & 2 ? 0x07030602u : 0x05010400u),
-                                 a & 1);
+              for (int j = 0; j < 4; ++j) {
+                if constexpr (CT == RWTTT_BF16) {
+                  wd[j] = __builtin_amdgcn_perm(vw[e][2 * j + 1][a / 2], vw[e][2 * j][a / 2],
+                                                a & 1 ? 0x07060302u : 0x05040100u);
+                } else {
+                  wd[j] = fp8_pair(__builtin_amdgcn_perm(vw[e][2 * j + 1][a / 4], vw[e][2 * j][a / 4],
+                                                         a & 2 ? 0x07030602u : 0x05010400u),
+                                   a & 1);
+                }
               }
-            }
-            const bf16x8_t val = as_bf16x8(wd);
+              const bf16x8_t val = as_bf16x8(wd);
 #pragma unroll
-            for (int b = NP - 1; b >= 0; --b)
-              acc[e * S::VE + a] =
-                  __builtin_amdgcn_mfma_f32_16x16x32_bf16(val, pt[b], acc[e * S::VE + a], 0, 0, 0);
-          }
+              for (int b = NP - 1; b >= 0; --b)
+                acc[e * S::VE + a] =
+                    __builtin_amdgcn_mfma_f32_16x16x32_bf16(val, pt[b], acc[e * S::VE + a], 0, 0, 0);
+            }
+        }
+        if (more) {
+          load_values(next);
+          at = next;
+        }
       }
-      if (more) {
-        load_values(next);
-        at = next;
-      }
-    }
     }
     if constexpr (!X) {
       l += __shfl_xor(l, 16);
