@@ -24,14 +24,18 @@ namespace {
 // A block takes some tokens, computes their sines and cosines once into LDS --
 // heads share them -- and passes over its part of the rows.  A lane owns whole
 // pairs, so a row may be turned in place: with HALF 16 bytes of each partner, with
-// INTERLEAVED 16 bytes.  Where a half of the turning channels is no whole number
-// of 16 bytes, a lane owns one pair.
+// INTERLEAVED 16 bytes.  Where a half of the turning channels is no whole number of
+// 16 bytes, the partners and the channels behind them are loaded and stored as they lie,
+// aligned to their type, and the pairs that are left over one by one.
 //
 // Bound by the bytes for a prefill: 8192 tokens of 32 + 8 heads of 128 channels in bf16
 // (168 MB in and out) take 33 us, 5.1 TB/s, the rate of a copy, and 27 us where the last-level
-// cache still holds some of them; a decode step of eight tokens 3.1 us.
+// cache still holds some of them; 4096 tokens of 100 turning channels (84 MB) 30 us, 44 with
+// a lane a pair; a decode step of eight tokens 3.1 us.
 
 constexpr int kRotThreads = 256;
+
+typedef u32x4_t Loose __attribute__((aligned(2)));
 
 template <int IO> struct IoRow {           // 16 bytes of io
   static constexpr int E = IO ? 8 : 4;
@@ -40,6 +44,17 @@ template <int IO> struct IoRow {           // 16 bytes of io
     const u32x4_t t = *reinterpret_cast<const u32x4_t*>(p);
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = t[i];
+  }
+  // anywhere that an element may be
+  __device__ __forceinline__ void load_loose(const char* p) {
+    const u32x4_t t = *reinterpret_cast<const Loose*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = t[i];
+  }
+  template <bool HINT> __device__ __forceinline__ void store_loose(char* p) const {
+    const u32x4_t t = {w[0], w[1], w[2], w[3]};
+    if (HINT) __builtin_nontemporal_store(t, reinterpret_cast<Loose*>(p));
+    else *reinterpret_cast<Loose*>(p) = t;
   }
   template <bool HINT> __device__ __forceinline__ void store(char* p) const {
     const u32x4_t t = {w[0], w[1], w[2], w[3]};
@@ -83,7 +98,7 @@ struct RotateParams {
 };
 
 // How the units of a head are laid out.
-enum class Turn { half, interleaved, pairs };   // pairs: HALF, one pair a unit
+enum class Turn { half, interleaved, ragged };   // ragged: HALF of any width
 
 // a b + c d, of fp32 io with one product's rounding taken back, so that the sum's remains.
 template <int IO> __device__ __forceinline__ float two_products(float a, float b, float c, float d) {
@@ -103,6 +118,8 @@ __global__ void __launch_bounds__(kRotThreads) kv_rotate_kernel(const RotatePara
   using M = Elem<std::conditional_t<IO, uint16_t, float>>;
   extern __shared__ float2 cs[];         // [tokens][turning / 2]: gain cos, gain sin
   const int half = p.turning / 2, n = int(p.n);
+  // ragged: units of pieces of pairs, of single pairs, of pieces behind them, of single channels
+  const int pieces = half / E, singles = pieces + half % E, behind = singles + (p.head_dim - p.turning) / E;
   const int t0 = blockIdx.x * rp.tokens, nt = min(rp.tokens, n - t0);
   const int u0 = blockIdx.y * rp.part, span = min(rp.per_token, u0 + rp.part) - u0, total = nt * span;
 
@@ -123,6 +140,7 @@ __global__ void __launch_bounds__(kRotThreads) kv_rotate_kernel(const RotatePara
       char* dst;
       const float2* at;
       int x;                             // -1: none
+      int kind;                          // of a ragged one
       IoRow<IO> a, b;
       float2 pair;
     } un[U];
@@ -131,6 +149,7 @@ __global__ void __launch_bounds__(kRotThreads) kv_rotate_kernel(const RotatePara
       Unit& w = un[j];
       const int i = i0 + j * kRotThreads;
       w.x = -1;
+      w.kind = 0;
       if (i >= total) continue;
       uint32_t u = i, x;                 // of one token a part of its units, of several all
       const int t = rp.tokens > 1 ? int(rp.whole(i, u)) : 0;
@@ -144,13 +163,25 @@ __global__ void __launch_bounds__(kRotThreads) kv_rotate_kernel(const RotatePara
       w.dst = static_cast<char*>(rows.out) + ((t0 + t) * rows.out_stride + size_t(h) * p.head_dim) * B;
       w.at = cs + t * half;
       if constexpr (T == Turn::half) {
-        const int pairs = half / E;
-        w.a.load(src + (w.x < pairs ? w.x : w.x + pairs) * 16);
-        if (w.x < pairs) w.b.load(src + half * B + w.x * 16);
+        w.a.load(src + (w.x < pieces ? w.x : w.x + pieces) * 16);
+        if (w.x < pieces) w.b.load(src + half * B + w.x * 16);
       } else if constexpr (T == Turn::interleaved) {
         w.a.load(src + w.x * 16);
+      } else if (w.x < pieces) {
+        w.a.load(src + w.x * 16);
+        w.b.load_loose(src + half * B + w.x * 16);
+      } else if (w.x < singles) {
+        w.x = pieces * E + (w.x - pieces);             // the pair's first channel
+        w.kind = 1;
+        w.pair = make_float2(M::get(src, w.x), M::get(src, w.x + half));
+      } else if (w.x < behind) {
+        w.x = p.turning + (w.x - singles) * E;         // the first channel
+        w.kind = 2;
+        w.a.load_loose(src + w.x * B);
       } else {
-        w.pair = make_float2(w.x < half ? M::get(src, w.x) : 0.f, M::get(src, w.x + half));
+        w.x = p.turning + (behind - singles) * E + (w.x - behind);
+        w.kind = 3;
+        w.pair.x = M::get(src, w.x);
       }
     }
     if (!waited) __syncthreads();
@@ -159,21 +190,23 @@ __global__ void __launch_bounds__(kRotThreads) kv_rotate_kernel(const RotatePara
     for (int j = 0; j < U; ++j) {
       Unit& w = un[j];
       if (w.x < 0) continue;
-      if constexpr (T == Turn::half) {
-        const int pairs = half / E;
-        if (w.x < pairs) {
-          IoRow<IO> ra, rb;
+      auto turn_pieces = [&](IoRow<IO>& ra, IoRow<IO>& rb) {
 #pragma unroll
-          for (int e = 0; e < E; e += 2) {
-            const float2 y0 = turned<IO>(make_float2(w.a.get(e), w.b.get(e)), w.at[w.x * E + e]);
-            const float2 y1 = turned<IO>(make_float2(w.a.get(e + 1), w.b.get(e + 1)), w.at[w.x * E + e + 1]);
-            ra.put_pair(e / 2, y0.x, y1.x);
-            rb.put_pair(e / 2, y0.y, y1.y);
-          }
+        for (int e = 0; e < E; e += 2) {
+          const float2 y0 = turned<IO>(make_float2(w.a.get(e), w.b.get(e)), w.at[w.x * E + e]);
+          const float2 y1 = turned<IO>(make_float2(w.a.get(e + 1), w.b.get(e + 1)), w.at[w.x * E + e + 1]);
+          ra.put_pair(e / 2, y0.x, y1.x);
+          rb.put_pair(e / 2, y0.y, y1.y);
+        }
+      };
+      if constexpr (T == Turn::half) {
+        if (w.x < pieces) {
+          IoRow<IO> ra, rb;
+          turn_pieces(ra, rb);
           ra.template store<HINT>(w.dst + w.x * 16);
           rb.template store<HINT>(w.dst + half * B + w.x * 16);
         } else {
-          w.a.template store<HINT>(w.dst + (w.x + pairs) * 16);
+          w.a.template store<HINT>(w.dst + (w.x + pieces) * 16);
         }
       } else if constexpr (T == Turn::interleaved) {
 #pragma unroll
@@ -185,14 +218,19 @@ __global__ void __launch_bounds__(kRotThreads) kv_rotate_kernel(const RotatePara
           }
         }
         w.a.template store<HINT>(w.dst + w.x * 16);
+      } else if (w.kind == 0) {
+        IoRow<IO> ra, rb;
+        turn_pieces(ra, rb);
+        ra.template store<HINT>(w.dst + w.x * 16);
+        rb.template store_loose<HINT>(w.dst + half * B + w.x * 16);
+      } else if (w.kind == 1) {
+        const float2 y = turned<IO>(w.pair, w.at[w.x]);
+        M::put(w.dst, w.x, y.x);
+        M::put(w.dst, w.x + half, y.y);
+      } else if (w.kind == 2) {
+        w.a.template store_loose<HINT>(w.dst + w.x * B);
       } else {
-        if (w.x < half) {
-          const float2 y = turned<IO>(w.pair, w.at[w.x]);
-          M::put(w.dst, w.x, y.x);
-          M::put(w.dst, w.x + half, y.y);
-        } else {
-          M::put(w.dst, w.x + half, w.pair.y);
-        }
+        M::put(w.dst, w.x, w.pair.x);
       }
     }
   }
@@ -280,7 +318,7 @@ template <int IO, int CT> hipError_t gather_dims(const GatherParams& p, hipStrea
 template <int IO, int U> hipError_t rotate_go(const RotateParams& p, Turn how, dim3 grid, size_t lds, hipStream_t stream) {
   auto kernel = how == Turn::half          ? kv_rotate_kernel<IO, Turn::half, U>
                 : how == Turn::interleaved ? kv_rotate_kernel<IO, Turn::interleaved, U>
-                                           : kv_rotate_kernel<IO, Turn::pairs, U>;
+                                           : kv_rotate_kernel<IO, Turn::ragged, U>;
   hipLaunchKernelGGL(kernel, grid, dim3(kRotThreads), lds, stream, p);
   return hipGetLastError();
 }
@@ -302,13 +340,13 @@ hipError_t launch_kv_rotate(const KvRotateLaunch& L, hipStream_t stream) {
   RotateParams p;
   p.L = L;
   const int E = L.io_bf16 ? 8 : 4, half = L.turning / 2;
-  const Turn how = L.interleaved ? Turn::interleaved : half % E == 0 ? Turn::half : Turn::pairs;
+  const Turn how = L.interleaved ? Turn::interleaved : half % E == 0 ? Turn::half : Turn::ragged;
   const bool in_place = (!L.q.heads || L.q.in == L.q.out) && (!L.k.heads || L.k.in == L.k.out);
   // in place the channels that do not turn are where they belong
   const int rest = in_place ? 0 : L.head_dim - L.turning;
   const int of_head = how == Turn::half          ? half / E + rest / E
                       : how == Turn::interleaved ? ((in_place ? L.turning : L.head_dim) + E - 1) / E
-                                                 : half + rest;
+                                                 : half / E + half % E + rest / E + rest % E;
   p.units = divider(uint32_t(of_head));
   p.per_token = of_head * (L.q.heads + L.k.heads);
   p.whole = divider(uint32_t(p.per_token));

@@ -64,7 +64,7 @@ POSITIONS = [0, 1, 2, 63, 1000, 4223, 131071, 8388607, 2 ** 31 - 1, 77]
 @pytest.mark.parametrize("io", ["bf16", "f32"])
 @pytest.mark.parametrize("layout", ["half", "interleaved"])
 @pytest.mark.parametrize("D,turning", [(64, 64), (128, 128), (256, 256), (128, 64), (64, 16), (256, 8), (64, 2), (128, 50),
-                                       (64, 34), (256, 250)])
+                                       (64, 34), (256, 250), (128, 20), (64, 62), (128, 126), (256, 14)])
 def test_rotation_matches_the_definition(io, layout, D, turning):
     """Whole heads, parts of them, halves that are no whole pieces; near and the farthest positions;
     queries and keys as strided parts of one projection, into outputs with strides of their own."""
