@@ -109,7 +109,7 @@ typedef struct rwttt_kv_config {
 } rwttt_kv_config;
 
 /* Bytes of device workspace of a handle: counters, partial results of the
- * attention's splits (the head layout fixes their number), and the page scores
+ * attention's splits (the types and the head layout fix their number), and the page scores
  * of at most 256 (owner, kv head) pairs.  Only the shape fields are read. */
 rwttt_status rwttt_kv_workspace_bytes(const rwttt_kv_config* cfg, size_t* bytes);
 

@@ -199,3 +199,38 @@ def test_rows_of_pages_swapped_for_junk():
     k, _ = gather(c.kv, [0, 1], [100, 7], i32([1 << 30, 40]), 1, 128, "bf16")
     assert torch.equal(k[1].double(), c.rows_of(1, 0, "k", [7]))
     c.close()
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("D,n", [(64, 5000), (128, 5000), (256, 3000)])
+def test_infinite_scores_anywhere_in_a_split_row(io, D, n):
+    """Products beyond fp32: one -inf score weighs nothing, -inf alone gives 0 and -inf, +inf and a
+    NaN block give NaN, each in the first rows, in the middle and in the last ones."""
+    places = [0, 1, n // 2, n - 2, n - 1]
+    cases = [(at, x) for at in places for x in ("-inf", "inf", "nan")] + [(None, "-inf")]
+    c = Cache4([n] * len(cases), H=1, G=1, D=D, page=16, io=io, seed=1, poison=False, bounds=False)
+    c.code["k"].fill_(1)
+    c.E["k"].fill_(125)
+    c.code["k"][..., 5] = 0
+    for r, (at, x) in enumerate(cases):
+        pages = c.table_h[r, :-(-n // 16)].long()
+        page, row = (pages, slice(None)) if at is None else (pages[at // 16], at % 16)
+        c.E["k"][page, 0, row, 0] = 255 if x == "nan" else 127 + 100
+        c.code["k"][page, 0, row, 5] = 15 if x == "-inf" else 7
+        c.code["k"][page, 0, row, :5] = 0
+        c.code["k"][page, 0, row, 6:32] = 0
+    c.close()
+    c.upload()
+    q = torch.ones((c.R, 1, D))
+    q[..., 5] = 2.0 ** 126                                   # one bf16 term
+    out, lse = c.attend(q=dev(q.to(DT[io])))
+    for r, (at, x) in enumerate(cases):
+        if at is None:
+            assert bool((out[r] == 0).all()) and float(lse[r, 0]) == -math.inf
+        elif x == "-inf":
+            v = c.rows_of(r, 0, "v", [j for j in range(n) if j != at]).mean(dim=0)
+            half = 2.0 ** -8 if io == "bf16" else 2.0 ** -24
+            assert bool(((out[r, 0].double() - v).abs() <= 1.01 * half * v.abs() + 1e-4).all())
+        else:
+            assert bool(torch.isnan(out[r]).all()) and bool(torch.isnan(lse[r]).all()), (at, x)
+    c.close()
