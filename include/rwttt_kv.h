@@ -168,6 +168,7 @@ rwttt_status rwttt_kv_extend(rwttt_kv* kv, const int32_t* have, const int32_t* w
  * The tokens of one page must be consecutive in the call (as rwttt_kv_extend
  * lists them), with no skipped slot between them; otherwise which of their
  * bounds remain is not specified.
+ * A slot that is named twice holds parts of either row.
  * n = 0 launches nothing.  One launch. */
 rwttt_status rwttt_kv_append(rwttt_kv* kv, uint32_t layer, const void* k, uint64_t k_stride,
                              const void* v, uint64_t v_stride, const int32_t* slots, uint32_t n,
