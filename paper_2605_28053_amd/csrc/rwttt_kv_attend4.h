@@ -21,7 +21,8 @@
 //
 // Bound by HBM for long rows, with the vector units half busy: 32 owners of 12000 to
 // 20000 rows, eight kv heads of four queries and 128 channels (540 MB) take 97 to 102 us,
-// 5.3 to 5.6 TB/s; the loads alone 88.  (Two terms of a probability, 16 bits, take as long.)
+// 5.3 to 5.6 TB/s; the loads alone 88.  (Two terms of a probability, 16 bits, take as
+// long, and 7% less at 64 channels.)
 // Of the steps: scores and values on one tile of
 // registers, page ids by scalar loads, probabilities split by rounding 111 us; ids from
 // lanes, cut probabilities, the scale within the exponent's product 103; the next tile's
