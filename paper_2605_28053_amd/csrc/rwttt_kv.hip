@@ -1147,7 +1147,7 @@ __device__ __forceinline__ bf16x8_t as_bf16x8(const uint32_t* w) {
 }
 
 // x = terms[0] + terms[1] + ... in bf16, eight values a lane: three terms keep all
-// 24 bits of each.
+// 24 bits of each.  For numbers from 0 to 1.
 template <int N> __device__ __forceinline__ void split_bf16(const float* x, bf16x8_t* terms) {
   float rest[8];
 #pragma unroll
@@ -1164,6 +1164,30 @@ template <int N> __device__ __forceinline__ void split_bf16(const float* x, bf16
       }
     }
     terms[t] = as_bf16x8(w);
+  }
+}
+
+// The same for any numbers, cut: a term is the next eight bits of x with x's sign.  So the
+// products of a key and the terms have one sign, and where they are beyond fp32 their
+// sum is the infinity that the whole product is (nearest terms have either sign, and
+// infinities of both are NaN together).  An infinity or a NaN is all in the first term.
+template <int N> __device__ __forceinline__ void cut_bf16(const float* x, bf16x8_t* terms) {
+  float rest[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) rest[i] = __builtin_canonicalizef(x[i]);   // a quiet NaN, whose upper half is one
+#pragma unroll
+  for (int t = 0; t < N; ++t) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[i] = __builtin_amdgcn_perm(__float_as_uint(rest[2 * i + 1]), __float_as_uint(rest[2 * i]), 0x07060302u);
+    terms[t] = as_bf16x8(w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float first = __uint_as_float(__float_as_uint(rest[i]) & 0xffff0000u);
+      // the maximum takes 0 for the NaN that is left of an infinity or a NaN
+      rest[i] = t == 0 ? copysignf(fmaxf(fabsf(rest[i]) - fabsf(first), 0.f), rest[i]) : rest[i] - first;
+    }
   }
 }
 
@@ -1375,7 +1399,7 @@ __global__ void __launch_bounds__(kAttThreads, blocks_a_cu(IO, CT, D)) kv_attend
 #pragma unroll
           for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(qw[s][j]);
           bf16x8_t terms[NQ];
-          split_bf16<NQ>(f, terms);
+          cut_bf16<NQ>(f, terms);
 #pragma unroll
           for (int k = 0; k < NQ; ++k) q[k][s] = terms[k];
         }
