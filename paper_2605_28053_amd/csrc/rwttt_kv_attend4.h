@@ -103,12 +103,13 @@ __device__ __forceinline__ void attend_rows4(const KvAttendLaunch& p, const Rows
   };
 
   // queries, negated if the scale is negative: column c is query c % heads of the tile's, as long
-  // as terms are left
+  // as terms are left.  A scale of zero makes them 0, or NaN where they are not finite, so that
+  // all scores of the rows that count are alike, and -inf stays that of the others.
   const bool used = c < heads * TG;
   const int column = used ? c % heads : 0, term = c / heads;
-  const uint32_t flip = scale_log2 < 0.f ? IO ? 0x80008000u : 0x80000000u : 0u;
-  // a scale of zero: all scores of the rows that count alike, and none of the others
-  const float to_log2 = scale_log2 == 0.f ? 0x1p-126f : fabsf(scale_log2);
+  const float sign = scale_log2 == 0.f ? 0.f : scale_log2 < 0.f ? -1.f : 1.f;
+  const uint32_t flip = scale_log2 < 0.f ? 0x80008000u : 0u;
+  const float to_log2 = scale_log2 == 0.f ? 1.f : fabsf(scale_log2);
   bf16x8_t q[NQ][QN];
 #pragma unroll
   for (int s = 0; s < QN; ++s) {
@@ -118,19 +119,25 @@ __device__ __forceinline__ void attend_rows4(const KvAttendLaunch& p, const Rows
     uint32_t w[IO ? 4 : 8];
 #pragma unroll
     for (int j = 0; j < (IO ? 4 : 8); j += 4) load_words<4>(src + j * 4, w + j);
-#pragma unroll
-    for (int j = 0; j < (IO ? 4 : 8); ++j) w[j] = used ? w[j] ^ flip : 0u;
     if constexpr (IO) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = used ? w[j] ^ flip : 0u;
       q[0][s] = as_bf16x8(w);
     } else {
       float f[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(w[j]);
+      for (int j = 0; j < 8; ++j) f[j] = used ? __uint_as_float(w[j]) * sign : 0.f;
       bf16x8_t terms[NQ];
       cut_bf16<NQ>(f, terms);
 #pragma unroll
       for (int k = 0; k < NQ; ++k) q[k][s] = terms[k];
     }
+  }
+  if (IO && scale_log2 == 0.f) {         // apart, so that other scales pay for a branch alone
+#pragma unroll
+    for (int s = 0; s < QN; ++s)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) q[0][s][i] = q[0][s][i] * static_cast<__bf16>(0.f);
   }
 
   const int k_lane = c * (D / 2) + g * (S::KE / 2), kp_lane = P * (D / 2) + g * S::KE / RWTTT_KV_BLOCK * P + c;
