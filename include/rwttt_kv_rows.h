@@ -81,7 +81,8 @@ rwttt_status rwttt_kv_rotate(rwttt_kv* kv, const rwttt_kv_rotary* rotary, const 
  * outside [0, n_owners) or whose position is outside [0, lengths[owner]) is
  * skipped: its rows of k and v are left as they were.  k or v may be NULL.
  * n = 0 launches nothing.  One launch.
- * Errors: RWTTT_E_INVALID as above, for outputs that overlap, or without k, v or table
+ * Errors: RWTTT_E_INVALID as above, for outputs that overlap each other or what the call
+ * may read (the arrays, the table, the layer's pages and scales), or without k, v or table
  * in the handle. */
 rwttt_status rwttt_kv_gather(rwttt_kv* kv, uint32_t layer, const int32_t* owners, const int32_t* positions,
                              const int32_t* lengths, uint32_t n, void* k, uint64_t k_stride, void* v,

@@ -98,6 +98,30 @@ bool overlap(const Rows& a, const Rows& b, uint64_t n, uint64_t bytes) {
   return apart < lower || step - apart < upper;
 }
 
+// An array that a call reads.
+struct Span {
+  const void* p;
+  uint64_t bytes;
+};
+
+// Whether some of n rows are also the array's; between two rows it may lie.
+bool overlap(const Rows& a, uint64_t n, uint64_t bytes, const Span& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  if (!b.p || y < x) return b.p && x - y < b.bytes;
+  if (y - x >= ((n - 1) * a.stride + a.row) * bytes) return false;
+  const uint64_t step = a.stride * bytes, at = (y - x) % step;
+  return at < a.row * bytes || step - at < b.bytes;
+}
+
+// Bytes of a layer's keys or values.
+uint64_t layer_bytes(const rwttt_kv_config& c) {
+  const uint64_t n = uint64_t(c.n_pages) * c.n_kv_heads * c.page_rows * c.head_dim;
+  return c.cache_dtype == RWTTT_F32    ? n * 4
+         : c.cache_dtype == RWTTT_BF16 ? n * 2
+         : c.cache_dtype == RWTTT_FP8  ? n
+                                       : n / 32 * 17;
+}
+
 rwttt_status hip_result(rwttt_kv* kv, hipError_t e) {
   if (e == hipSuccess) return RWTTT_OK;
   kv->last_hip = static_cast<int32_t>(e);
@@ -232,8 +256,19 @@ rwttt_status rwttt_kv_gather(rwttt_kv* kv, uint32_t layer, const int32_t* owners
   if (k && (misaligned(k, 16) || !stride_ok(kv, k_stride, heads))) return RWTTT_E_INVALID;
   if (v && (misaligned(v, 16) || !stride_ok(kv, v_stride, heads))) return RWTTT_E_INVALID;
   const uint64_t row = uint64_t(heads) * kv->cfg.head_dim;
-  if (k && v && overlap(Rows{k, k_stride, row}, Rows{v, v_stride, row}, n, type_bytes(kv->cfg.io_dtype)))
-    return RWTTT_E_INVALID;
+  const uint64_t io_bytes = type_bytes(kv->cfg.io_dtype);
+  if (k && v && overlap(Rows{k, k_stride, row}, Rows{v, v_stride, row}, n, io_bytes)) return RWTTT_E_INVALID;
+  const Span read[] = {{owners, n * 4ull},
+                       {positions, n * 4ull},
+                       {lengths, kv->cfg.n_owners * 4ull},
+                       {kv->cfg.table, uint64_t(kv->cfg.n_owners) * kv->cfg.max_pages * 4},
+                       {kv->k[layer], layer_bytes(kv->cfg)},
+                       {kv->v[layer], layer_bytes(kv->cfg)},
+                       {head_scale(kv, kv->cfg.k_scale, layer), heads * 4ull},
+                       {head_scale(kv, kv->cfg.v_scale, layer), heads * 4ull}};
+  for (const Span& a : read)
+    if ((k && overlap(Rows{k, k_stride, row}, n, io_bytes, a)) || (v && overlap(Rows{v, v_stride, row}, n, io_bytes, a)))
+      return RWTTT_E_INVALID;
   rwttt::KvGatherLaunch L;
   L.s = kv->shape;
   L.k = kv->k[layer];

@@ -111,6 +111,45 @@ def test_rotate_refuses_a_bad_rotary(args):
     KV.rwttt_kv_destroy(kv)
 
 
+# outputs of three rows of 512 bytes, at A[13] and A[14], 512 apart unless said
+AT_K, AT_V, WIDE = A[13], A[14], dict(k_stride=1024, v_stride=1024)
+
+
+@pytest.mark.parametrize("kw", [
+    # the first and the last byte of either output, from below and from within
+    dict(owners=AT_K), dict(owners=AT_K - 16, n=5), dict(owners=AT_K + 1536 - 16), dict(owners=AT_V + 512),
+    dict(positions=AT_K), dict(positions=AT_V + 1536 - 16), dict(positions=AT_V - 16, n=5), dict(lengths=AT_V), dict(lengths=AT_K + 16),
+    # between rows that are apart, where an array reaches the next one
+    dict(**WIDE, owners=AT_K + 2048 - 16, n=5), dict(**WIDE, positions=AT_V + 2048 - 16, n=5)])
+def test_gather_refuses_outputs_over_what_it_reads(kw):
+    kv = create()
+    assert KV.rwttt_kv_gather(kv, **{**GATHER, **kw}) == R.RWTTT_E_INVALID
+    KV.rwttt_kv_destroy(kv)
+
+
+CACHE = 100 * 2 * 64 * 128 * 17 // 32           # bytes of a layer's keys or values
+TABLE = 4 * 16 * 4
+
+
+@pytest.mark.parametrize("kw", [
+    dict(k=A[3]), dict(v=A[5]), dict(k=A[5]), dict(v=A[3]), dict(k=A[3] + CACHE - 16), dict(v=A[5] - 1536 + 16),
+    dict(k=A[0]), dict(v=A[0] + TABLE - 16), dict(k=A[0] - 1536 + 16), dict(v=0, k=A[5] + 4096), dict(k=0, v=A[3] + 4096)])
+def test_gather_refuses_outputs_over_the_pages_or_the_table(kw):
+    kv = create()
+    assert KV.rwttt_kv_gather(kv, **{**GATHER, **kw}) == R.RWTTT_E_INVALID
+    KV.rwttt_kv_destroy(kv)
+
+
+@pytest.mark.parametrize("scale", ["k_scale", "v_scale"])
+@pytest.mark.parametrize("side", ["k", "v"])
+def test_gather_refuses_outputs_over_the_scales(scale, side):
+    kv = create(cache_dtype=KV.RWTTT_FP8, k_scale=A[16], v_scale=A[17])
+    at = A[16] if scale == "k_scale" else A[17]
+    assert KV.rwttt_kv_gather(kv, **{**GATHER, side: at}) == R.RWTTT_E_INVALID
+    assert KV.rwttt_kv_gather(kv, **{**GATHER, side: at - 1536 + 16}) == R.RWTTT_E_INVALID
+    KV.rwttt_kv_destroy(kv)
+
+
 # ---------------------------------------------------------------------------
 # frequencies
 # ---------------------------------------------------------------------------
