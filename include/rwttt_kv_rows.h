@@ -68,8 +68,9 @@ rwttt_status rwttt_kv_turns(uint32_t turning, double base, int32_t scaling, doub
  * infinite channel makes its pair what the two products and their sum are.
  * Needs no buffer of the handle but its shape; n = 0 launches nothing.  One launch.
  * Errors: RWTTT_E_INVALID for a bad rotary, null or misaligned pointers, a bad
- * stride, an output that overlaps an input or the other output other than as said
- * (rows of different strides count as overlapping where the spans of all n meet). */
+ * stride, an output that overlaps an input (positions and turns among them) or the other
+ * output other than as said (rows of different strides count as overlapping where the spans
+ * of all n meet). */
 rwttt_status rwttt_kv_rotate(rwttt_kv* kv, const rwttt_kv_rotary* rotary, const int32_t* positions, uint32_t n,
                              const void* q, uint64_t q_stride, void* q_out, uint64_t q_out_stride,
                              const void* k, uint64_t k_stride, void* k_out, uint64_t k_out_stride, void* stream);

@@ -403,6 +403,10 @@ rwttt_status rwttt_kv_rotate(rwttt_kv* kv, const rwttt_kv_rotary* rotary, const 
       if (!itself && overlap(out, Rows{b.in, b.stride, row_b}, n, bytes)) return RWTTT_E_INVALID;
       if (&a != &b && overlap(out, Rows{b.out, b.out_stride, row_b}, n, bytes)) return RWTTT_E_INVALID;
     }
+  const Span read[] = {{positions, n * 4ull}, {rotary->turns, rotary->turning / 2 * 8ull}};
+  for (const Side& a : sides)
+    for (const Span& b : read)
+      if (a.in && overlap(Rows{a.out, a.out_stride, uint64_t(a.heads) * c.head_dim}, n, bytes, b)) return RWTTT_E_INVALID;
   rwttt::KvRotateLaunch L;
   L.io_bf16 = kv->shape.io_bf16;
   L.head_dim = kv->shape.head_dim;

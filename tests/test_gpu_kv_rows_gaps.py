@@ -5,7 +5,8 @@ import torch
 
 from paper_2605_28053_amd import _rwttt_kv as KV
 from tests.kv4_util import Cache4
-from tests.kv_util import ok, stream
+from tests.kv_util import dev, i32, ok, stream
+from tests.test_gpu_rotary import Rotor
 
 pytestmark = pytest.mark.gpu
 
@@ -38,3 +39,22 @@ def test_gather_between_rows():
             assert bool((got == 7.0).all()) if want is None else torch.equal(got[None], want), (x, i)
     assert all(torch.equal(b[:, 128:].view(torch.int16), a.view(torch.int16)) for a, b in zip(before, (k_buf, v_buf)))
     c.close()
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+def test_rotate_between_rows(in_place):
+    f = Rotor(2, 1, 64, 64, "half", "bf16")
+    pos, x = [5, -1, 100000, 0], torch.randn((4, 128), generator=torch.Generator().manual_seed(1)).bfloat16()
+    buf, q, between = rows_with_gaps(4, 128, 320, 7.0)
+    q.copy_(x)
+    src = q if in_place else dev(x)
+    at, table = between(0, pos), between(2, f.units[:32], torch.uint64)
+    before = buf[:, 128:].clone()
+    rot = KV.make_rotary(64, KV.RWTTT_ROTARY_HALF, table.data_ptr())
+    ok(KV.rwttt_kv_rotate(f.kv, rot, at.data_ptr(), 4, src.data_ptr(), src.stride(0), q.data_ptr(), q.stride(0), 0, 0, 0, 0,
+                          stream()))
+    want = dev(x).view(4, 2, 64)
+    f(i32(pos), q=want, q_out=want)
+    torch.cuda.synchronize()
+    assert torch.equal(q, want.view(4, 128)) and torch.equal(buf[:, 128:].view(torch.int16), before.view(torch.int16))
+    f.close()

@@ -111,7 +111,7 @@ def test_rotate_refuses_a_bad_rotary(args):
     KV.rwttt_kv_destroy(kv)
 
 
-# outputs of three rows of 512 bytes, at A[13] and A[14], 512 apart unless said
+# outputs of three rows of 512 bytes, at A[13] and A[14], 512 apart unless said; queries' rows are of 2048
 AT_K, AT_V, WIDE = A[13], A[14], dict(k_stride=1024, v_stride=1024)
 
 
@@ -147,6 +147,29 @@ def test_gather_refuses_outputs_over_the_scales(scale, side):
     at = A[16] if scale == "k_scale" else A[17]
     assert KV.rwttt_kv_gather(kv, **{**GATHER, side: at}) == R.RWTTT_E_INVALID
     assert KV.rwttt_kv_gather(kv, **{**GATHER, side: at - 1536 + 16}) == R.RWTTT_E_INVALID
+    KV.rwttt_kv_destroy(kv)
+
+
+AT_Q, ROWS3 = A[12], 3 * 2 * Q                  # q_out: three rows of 2048 bytes
+
+
+@pytest.mark.parametrize("kw", [
+    dict(positions=AT_Q), dict(positions=AT_Q + ROWS3 - 16), dict(positions=AT_Q - 16, n=5), dict(positions=A[14]),
+    dict(positions=A[14] + 3 * 2 * K - 16), dict(positions=A[11], q_out=A[11]), dict(positions=A[13] + 512, k_out=A[13]),
+    dict(q=0, q_out=0, positions=A[14] + 512), dict(k=0, k_out=0, positions=AT_Q + 2048),
+    # the queries of one projection turned in place: the place of keys and values is free, the next row is not
+    dict(**PARTS, q_out=A[11], q_out_stride=STRIDE, n=300, positions=A[11] + 2 * Q)])
+def test_rotate_refuses_outputs_over_the_positions(kw):
+    kv = create()
+    assert KV.rwttt_kv_rotate(kv, KV.make_rotary(128, 0, A[15]), **{**ROTATE, **kw}) == R.RWTTT_E_INVALID
+    KV.rwttt_kv_destroy(kv)
+
+
+@pytest.mark.parametrize("turns", [AT_Q, AT_Q + ROWS3 - 16, AT_Q - 512 + 16, A[14], A[14] + 3 * 2 * K - 16, A[14] - 512 + 16])
+def test_rotate_refuses_outputs_over_the_table(turns):
+    """Of 64 pairs: 512 bytes."""
+    kv = create()
+    assert KV.rwttt_kv_rotate(kv, KV.make_rotary(128, 1, turns), **ROTATE) == R.RWTTT_E_INVALID
     KV.rwttt_kv_destroy(kv)
 
 
