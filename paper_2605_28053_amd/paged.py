@@ -154,7 +154,8 @@ class PagedCache:
         """Turn queries and keys [n, heads, head_dim] to their positions; in place unless q_out or k_out is given.
 
         ``positions`` (int32 [n]) are the open step's, in slot order, if not given; tokens of
-        negative ones are left as they are.  Returns (q_out, k_out)."""
+        negative ones are left as they are.  Returns (q_out, k_out), which autograd knows nothing
+        of: ``rotary.inverse()`` turns their gradients to those of q and k."""
         if q is None and k is None:
             raise ValueError("queries or keys")
         if (q is None and q_out is not None) or (k is None and k_out is not None):
@@ -169,6 +170,7 @@ class PagedCache:
                 raise ValueError("more rows than a step may add")
             positions = self.positions[:n]
         self._index(positions, n)
+        self._written(q_out=q_out, k_out=k_out)
         args = []
         for t, heads, name in ((q, self.n_heads, "q"), (q_out, self.n_heads, "q_out"), (k, self.n_kv_heads, "k"),
                                (k_out, self.n_kv_heads, "k_out")):
@@ -199,6 +201,7 @@ class PagedCache:
         k = torch.zeros(shape, dtype=dtype, device=self.device) if k is None else k
         v = torch.zeros(shape, dtype=dtype, device=self.device) if v is None else v
         k_stride, v_stride = self._rows(k, self.n_kv_heads, "k", n), self._rows(v, self.n_kv_heads, "v", n)
+        self._written(k=k, v=v)
         _check(KV.rwttt_kv_gather(self.kv, layer, owners.data_ptr(), positions.data_ptr(), self.now().data_ptr(), n,
                                   k.data_ptr(), k_stride, v.data_ptr(), v_stride, _stream()), "rwttt_kv_gather")
         return k, v
@@ -265,6 +268,13 @@ class PagedCache:
     def _here(self, t, name):
         if t.device != self.lengths.device:
             raise ValueError(f"{name} is on {t.device}, the cache on {self.lengths.device}")
+
+    @staticmethod
+    def _written(**tensors):
+        """Autograd does not see a call's writes, so it must not hold gradients for what they replace."""
+        for name, t in tensors.items():
+            if t is not None and t.requires_grad and torch.is_grad_enabled():
+                raise ValueError(f"{name} requires a gradient: give an output of its own, or call under torch.no_grad()")
 
     def _dense(self, t, dtype, shape, name):
         self._here(t, name)

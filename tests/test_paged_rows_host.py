@@ -123,3 +123,23 @@ def test_gather_marshals_and_refuses(calls):
     assert len(calls) == made
     k, v = c.gather(0, owners[:0], positions[:0])
     assert tuple(k.shape) == (0, 2, 64) and calls[-1][1][5] == 0
+
+
+def test_outputs_that_require_a_gradient_are_refused(calls):
+    """Autograd does not see what the calls write: its gradients would be those of the values before."""
+    c, r, at = cache(), rotary(), torch.zeros(2, dtype=I32)
+    q, k = rows(2, 4, 64).requires_grad_(), rows(2, 2, 64)
+    bad = [lambda: c.rotate(r, q, k, at), lambda: c.rotate(r, q=rows(2, 4, 64), positions=at, q_out=q),
+           lambda: c.rotate(r, q=q * 2, positions=at), lambda: c.rotate(r, k=k.clone().requires_grad_(), positions=at),
+           lambda: c.gather(0, at, at, k=k.clone().requires_grad_()), lambda: c.gather(0, at, at, v=k.clone().requires_grad_())]
+    made = len(calls)
+    for call in bad:
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+    assert len(calls) == made
+    with torch.no_grad():
+        for call in bad:
+            call()
+    out = rows(2, 4, 64)
+    assert c.rotate(r, q=q, positions=at, q_out=out) == (out, None) and not out.requires_grad
+    assert c.rotate(r, q=q.detach(), positions=at)[0] is not None
