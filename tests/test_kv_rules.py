@@ -108,3 +108,22 @@ def test_the_hint_goes_by_the_most_a_call_can_read(ask):
     assert not hint(keep=128) and hint(keep=129) and not hint(keep=2000, max_pages=100)
     # a window of 16 * 127 + 1 rows touches 128 pages where it begins in a page's last row, of 16 * 127 + 2 one more
     assert not hint(window=16 * 127 + 1) and hint(window=16 * 127 + 2) and hint(window=1 << 23)
+
+
+@pytest.mark.parametrize("blocks", [256, 512, 768])
+@pytest.mark.parametrize("tile", [16, 32, 64])
+@pytest.mark.parametrize("longest", [16, 48, 64, 256, 4096, 65536])
+def test_every_tile_is_held_for_any_number_of_blocks(ask, blocks, tile, longest):
+    """The same for three blocks a CU and tiles of 64 rows, and no more blocks launched than a call may have."""
+    rng = random.Random(blocks + tile + longest)
+    lines = []
+    for n in (1, 2, 5, 8, 65, 480, 800):
+        for vh in (1, 3, 8, 24):
+            if n * vh > 2000 or n * vh * longest > 1 << 22:
+                continue
+            for lens in ([longest] * n, [1] * n, [rng.choice([0, 1, 15, 16, 17, 63, 64, 65, rng.randint(0, longest)]) % (longest + 1)
+                                                  for _ in range(n)]):
+                lines.append(f"cut {blocks} {vh} {tile} {longest} {n} {' '.join(map(str, lens))}")
+    assert len(lines) > 8
+    for line, (grid, parts, lost, wrong, joins) in zip(lines, ask(lines)):
+        assert (lost, wrong, joins) == (0, 0, 0) and 1 <= grid <= blocks and parts <= grid, line[:80]
