@@ -1171,16 +1171,20 @@ template <int N> __device__ __forceinline__ void split_bf16(const float* x, bf16
 // products of a key and the terms have one sign, and where they are beyond fp32 their
 // sum is the infinity that the whole product is (nearest terms have either sign, and
 // infinities of both are NaN together).  An infinity or a NaN is all in the first term.
-template <int N> __device__ __forceinline__ void cut_bf16(const float* x, bf16x8_t* terms) {
+// FULL: for keys that may be infinite.  A term without bits, whose product with one would
+// be NaN, is x 2^-40 instead, which no sum in fp32 shows (of queries from 2^-86 on: then it is
+// a normal number); below the bits of other terms it is cut off.
+template <int N, bool FULL> __device__ __forceinline__ void cut_bf16(const float* x, bf16x8_t* terms) {
   float rest[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) rest[i] = __builtin_canonicalizef(x[i]);   // a quiet NaN, whose upper half is one
 #pragma unroll
   for (int t = 0; t < N; ++t) {
-    uint32_t w[4];
+    uint32_t w[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      w[i] = __builtin_amdgcn_perm(__float_as_uint(rest[2 * i + 1]), __float_as_uint(rest[2 * i]), 0x07060302u);
+    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(FULL && t ? fmaf(x[i], 0x1p-40f, rest[i]) : rest[i]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x07060302u);
     terms[t] = as_bf16x8(w);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -1399,7 +1403,7 @@ __global__ void __launch_bounds__(kAttThreads, blocks_a_cu(IO, CT, D)) kv_attend
 #pragma unroll
           for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(qw[s][j]);
           bf16x8_t terms[NQ];
-          cut_bf16<NQ>(f, terms);
+          cut_bf16<NQ, CT == RWTTT_BF16>(f, terms);
 #pragma unroll
           for (int k = 0; k < NQ; ++k) q[k][s] = terms[k];
         }

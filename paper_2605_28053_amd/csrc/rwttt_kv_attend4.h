@@ -128,7 +128,7 @@ __device__ __forceinline__ void attend_rows4(const KvAttendLaunch& p, const Rows
 #pragma unroll
       for (int j = 0; j < 8; ++j) f[j] = used ? __uint_as_float(w[j]) * sign : 0.f;
       bf16x8_t terms[NQ];
-      cut_bf16<NQ>(f, terms);
+      cut_bf16<NQ, false>(f, terms);
 #pragma unroll
       for (int k = 0; k < NQ; ++k) q[k][s] = terms[k];
     }

@@ -81,3 +81,32 @@ def test_queries_that_are_not_finite(cache, D):
     for r in (1, 2, 3):
         assert bool(torch.isnan(out[r]).all()) and math.isnan(float(lse[r, 0])), r
     c.close()
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("x", [1.0, -1.0, 1 + 2.0 ** -9, 0.3, -2.0 ** -60, 2.0 ** 100])
+def test_infinite_keys(D, x):
+    """Stored in bf16, against queries of one, two and three terms: -inf in a row weighs nothing, in all rows
+    it gives 0 and -inf, +inf and a NaN give NaN, and behind the rows they have no influence."""
+    kinds = [("low", [AT]), ("low", [0]), ("low", [N - 1]), ("low", range(N)), ("high", [AT]), ("nan", [AT])]
+    c = build("bf16", D, len(kinds), {})
+    k = c.kd.cpu()
+    # -inf where the product with x is
+    value = {"low": -math.inf if x > 0 else math.inf, "high": math.inf if x > 0 else -math.inf, "nan": math.nan}
+    k[torch.isnan(k)] = math.inf
+    for r, (kind, rows) in enumerate(kinds):
+        for j in rows:
+            k[int(c.table_h[r, j // 16]), 0, j % 16, CHANNEL] = value[kind]
+    c.kd.copy_(k)
+    q = torch.ones((len(kinds), 1, D))
+    q[:, 0, CHANNEL] = x
+    out, lse = c.attend(q=dev(q))
+    for r, (kind, rows) in enumerate(kinds):
+        if kind != "low":
+            assert bool(torch.isnan(out[r]).all()) and math.isnan(float(lse[r, 0])), r
+        elif len(rows) == N:
+            assert bool((out[r] == 0).all()) and float(lse[r, 0]) == -math.inf, r
+        else:
+            v = c.rows_of(r, 0, "v", [j for j in range(N) if j not in rows])
+            assert bool(((out[r, 0].double() - v.mean(dim=0)).abs() <= 200 * 2.0 ** -24 * v.abs().amax()).all()), r
+    c.close()
