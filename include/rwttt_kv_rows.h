@@ -24,8 +24,9 @@ extern "C" {
  * with (a, b) channels i and i + turning / 2 (RWTTT_ROTARY_HALF) or 2 i and 2 i + 1
  * (RWTTT_ROTARY_INTERLEAVED); the head's other channels stay as they are.
  * Frequencies are kept in turns: turns[i] is w_i / 2 pi in units of 2^-64, so that
- * the angle of any position is a 64-bit product that wraps at whole turns, off by at most
- * p 2^-65 turns. */
+ * the angle of any position is a 64-bit product that wraps at whole turns, off by p times
+ * what turns[i] is off by: half a unit in a table of nearest numbers, and in that of
+ * rwttt_kv_turns at most 1 + 24 w_i / 2 pi units (below 5 where w_i is at most 1). */
 #define RWTTT_ROTARY_HALF        0
 #define RWTTT_ROTARY_INTERLEAVED 1
 
@@ -78,7 +79,7 @@ rwttt_status rwttt_kv_rotate(rwttt_kv* kv, const rwttt_kv_rotary* rotary, const 
 /* Read n stored rows back: row i of k and of v ([n, n_kv_heads, head_dim], io type,
  * rows k_stride and v_stride elements apart) is position positions[i] of owner
  * owners[i] ([n] each, as rwttt_kv_extend lists them), rounded once to the io type
- * (exact but for RWTTT_FP8 with scales, and a fp32 value in bf16).  A pair whose owner is
+ * (exact but for RWTTT_FP8 with scales).  A pair whose owner is
  * outside [0, n_owners) or whose position is outside [0, lengths[owner]) is
  * skipped: its rows of k and v are left as they were.  k or v may be NULL.
  * n = 0 launches nothing.  One launch.

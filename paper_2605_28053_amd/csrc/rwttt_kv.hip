@@ -1047,10 +1047,12 @@ constexpr int kAttWaves = kAttThreads / 64;
 constexpr int kJoinWindow = 32, kJoinDirect = 48;
 constexpr int kAttPad = 4;               // floats behind a query's sums in LDS: neighbours in other banks
 
-// Rows of keys a wave takes at a time.  Of 4 bits (540 MB at 128 channels, 280 at 64):
+// Rows of keys a wave takes at a time.  Of 4 bits (540 MB at 128 channels, 280 at 64, each
+// read again and again):
 // 97 us with 32 rows and three blocks a CU, 99 with 64 and two, 105 with 32 and two;
-// 62.6 us with 64 rows and three blocks, 66 with 32 and three or four; at 256 channels
-// 59.5 us with 32 rows, 62.5 with 64.
+// 62.6 us with 64 rows and three blocks (70 where three such caches take turns, so that all
+// comes from memory), 66 with 32 and three or four; at 256 channels 59.5 us with 32 rows,
+// 62.5 with 64.
 constexpr int tile_rows(int ct, int dim) {
   return ct == RWTTT_FP4 ? (dim == 64 ? 64 : 32) : ct == RWTTT_F32 ? 16 : 32;
 }
@@ -1058,7 +1060,10 @@ constexpr int tile_rows(int ct, int dim) {
 // Blocks of a call that a CU holds, and the chip.  What the registers leave room for:
 // at 256 channels no more than one (16 owners of 8500 rows: 180 us in bf16 and 94 in
 // e4m3 so, 184 and 102 with twice the blocks; two of 4 bits take 57.7 us instead of
-// 59.5, but 20.8 instead of 19.0 over selected pages).
+// 59.5, but 20.8 instead of 19.0 over selected pages).  fp32 queries over 4 bits at 64
+// channels do not quite fit three blocks, 2 to 8 registers of a lane are spilled before the
+// tiles: the 280 MB above take 70 us so and 73 with two blocks, eight owners of 4200 rows
+// 16.1 and 14.9.
 constexpr int blocks_a_cu(int io, int ct, int dim) {
   if (dim == 256) return 1;
   return ct == RWTTT_FP4 && (io || dim == 64) ? 3 : 2;

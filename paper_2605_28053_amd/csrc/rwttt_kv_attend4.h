@@ -20,9 +20,10 @@
 // probabilities is a product with ones.
 //
 // Bound by HBM for long rows, with the vector units half busy: 32 owners of 12000 to
-// 20000 rows, eight kv heads of four queries and 128 channels (540 MB) take 97 to 102 us,
-// 5.3 to 5.6 TB/s; the loads alone 88.  (Two terms of a probability, 16 bits, take as
-// long, and 7% less at 64 channels.)
+// 20000 rows, eight kv heads of four queries and 128 channels (540 MB) take 95 to 105 us,
+// 5.1 to 5.7 TB/s, by how much of them the last-level cache still holds; the loads alone 88.
+// (Two terms of a probability, 16 bits, would take 2% less, 2 to 4% at 256 channels, 2 to 5%
+// at 64.)
 // Of the steps: scores and values on one tile of
 // registers, page ids by scalar loads, probabilities split by rounding 111 us; ids from
 // lanes, cut probabilities, the scale within the exponent's product 103; the next tile's
